@@ -13,6 +13,8 @@ Entry points (same names as the C ABI):
   cq_family_supported, cq_gemm_model_dtype_family, cq_gemm_a8_family,
   cq_select_set, cq_select_query, cq_probe_read and cq_probe_wide_rows (measurement aids,
   include/cq_measure.h)
+The operators between the packed products (norms, rotary append, paged
+attention; include/cq_block.h) are bound in ``block.py`` and exported here.
 The measured kernel-selection tuner that fills the selection table is in
 ``selection.py``.
 """
@@ -35,7 +37,8 @@ EXPORTS = ("cq_status_str", "cq_pack_groups", "cq_decode_ref", "cq_gemm_model_dt
            "cq_gemm_routed_model_dtype", "cq_set_gemv_max_rows", "cq_get_gemv_max_rows",
            "cq_family_supported", "cq_gemm_model_dtype_family", "cq_gemm_a8_family", "cq_select_set",
            "cq_select_query", "cq_probe_read", "cq_gemm_routed_model_dtype_noalloc", "cq_set_a8_fused_launch",
-           "cq_get_a8_fused_launch", "cq_probe_wide_rows")
+           "cq_get_a8_fused_launch", "cq_probe_wide_rows", "cq_norm_residual", "cq_norm_residual_a8",
+           "cq_rope_append", "cq_attn_paged", "cq_attn_shared_prefix", "cq_attn_workspace_bytes")
 
 CQ_PATH_MODEL_DTYPE, CQ_PATH_A8 = 0, 1
 FAMILIES = {"auto": 0, "gemv_stream": 1, "gemv_lut": 2, "gemv_narrow": 3, "gemv_generic": 4, "gemm_mfma": 5,
@@ -122,6 +125,7 @@ def lib() -> ctypes.CDLL:
     L.cq_probe_wide_rows.argtypes = [i32, ctypes.POINTER(cq_weight), i64]
     L.cq_probe_read.restype = ctypes.c_int
     L.cq_probe_read.argtypes = [vp, i64, vp, vp]
+    block.declare(L)
     _lib = L
     return L
 
@@ -446,3 +450,16 @@ def cq_probe_read(buf, sink, stream=None):
 def cq_probe_wide_rows(path: int, w, m: int) -> int:
     """x-tile height that the wide GEMM of ``path`` takes for m rows (0: it does not take them)."""
     return lib().cq_probe_wide_rows(path, ctypes.byref(w if isinstance(w, cq_weight) else w.desc), m)
+
+
+# ---------------------------------------------------------------- between the packed products
+
+from . import block  # noqa: E402
+from .block import (  # noqa: E402,F401
+    cq_attn_paged,
+    cq_attn_shared_prefix,
+    cq_attn_workspace_bytes,
+    cq_norm_residual,
+    cq_norm_residual_a8,
+    cq_rope_append,
+)

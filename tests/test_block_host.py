@@ -1,0 +1,156 @@
+"""Host-side checks of the operators between the packed products (no GPU): every
+bad argument is refused, by its status, before any device work."""
+import ctypes
+
+import pytest
+
+import paper_2608_06763_amd as cq
+from paper_2608_06763_amd.block import cq_attn_args, cq_kv_cache, cq_norm_args, cq_rope_args
+
+OK, BAD = 4096, 4100  # a 16-byte aligned address that nothing reads, and one that is not aligned
+
+
+def ref(x):
+    return ctypes.byref(x)
+
+
+def norm(**kw):
+    a = dict(y=OK, post_weight=OK, gate=OK, residual=OK, weight=OK, residual_out=OK, out=OK, gate_stride=64, rows=3,
+             width=64, dtype=0, residual_dtype=0, alpha=1.0, eps=1e-5, weight_offset=0.0)
+    a.update(kw)
+    return cq_norm_args(**a)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(residual=None), 1), (dict(weight=None), 1), (dict(out=None), 1), (dict(rows=0), 1), (dict(width=0), 1),
+    (dict(y=None), 1), (dict(y=None, post_weight=None), 1), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1),
+    (dict(alpha=float("inf")), 1), (dict(weight_offset=float("nan")), 1), (dict(width=60), 2), (dict(width=32776), 2),
+    (dict(rows=1 << 31), 2), (dict(gate_stride=56), 2), (dict(gate_stride=68), 2), (dict(gate_stride=-64), 2),
+    (dict(gate_stride=1 << 41), 2), (dict(dtype=2), 6), (dict(residual_dtype=1), 6), (dict(residual_dtype=5), 6),
+] + [({f: BAD}, 3) for f in ("y", "post_weight", "gate", "residual", "weight", "residual_out", "out")])
+def test_norm_refusals(kw, want):
+    L = cq.lib()
+    assert L.cq_norm_residual(ref(norm(**kw)), None) == want
+    if kw != dict(out=None):
+        assert L.cq_norm_residual_a8(ref(norm(**kw)), OK, OK, None) == want
+
+
+def test_norm_a8_refusals():
+    L = cq.lib()
+    assert L.cq_norm_residual(None, None) == 1
+    assert L.cq_norm_residual_a8(ref(norm()), None, OK, None) == 1
+    assert L.cq_norm_residual_a8(ref(norm()), OK, None, None) == 1
+    assert L.cq_norm_residual_a8(ref(norm(width=72, gate_stride=72)), OK, OK, None) == 2
+    assert L.cq_norm_residual_a8(ref(norm()), BAD, OK, None) == 3
+    assert L.cq_norm_residual_a8(ref(norm()), OK, BAD, None) == 3
+
+
+def cache(**kw):
+    a = dict(dtype=0, kv_heads=2, dim=64, page=16, pages=10, k=OK, v=OK)
+    a.update(kw)
+    return cq_kv_cache(**a)
+
+
+BAD_CACHES = [(dict(k=None), 1), (dict(v=None), 1), (dict(kv_heads=0), 1), (dict(pages=0), 1), (dict(dtype=2), 6),
+              (dict(dim=96), 8), (dict(dim=32), 8), (dict(page=8), 2), (dict(page=48), 2), (dict(page=2048), 2),
+              (dict(pages=1 << 27), 2), (dict(kv_heads=70000), 2), (dict(k=BAD), 3), (dict(v=BAD), 3)]
+
+
+def rope(**kw):
+    a = dict(q=OK, k=OK, v=OK, q_out=OK, q_stride=256, k_stride=128, v_stride=128, q_out_stride=256, cos=OK, sin=OK,
+             positions=OK, slots=OK, tokens=5, table_rows=9, heads=4, rot=64, interleaved=0)
+    a.update(kw)
+    return cq_rope_args(**a)
+
+
+@pytest.mark.parametrize("kw,want", [({f: None}, 1) for f in ("q", "k", "v", "q_out", "cos", "sin", "positions", "slots")] + [
+    (dict(tokens=0), 1), (dict(heads=0), 1), (dict(table_rows=0), 1), (dict(interleaved=2), 1), (dict(rot=-16), 1),
+    (dict(rot=80), 2), (dict(rot=24), 2), (dict(tokens=1 << 31), 2), (dict(q_stride=248), 2), (dict(q_stride=260), 2),
+    (dict(k_stride=120), 2), (dict(v_stride=132), 2), (dict(q_out_stride=264), 2), (dict(q_stride=1 << 41), 2),
+] + [({f: BAD}, 3) for f in ("q", "k", "v", "q_out", "cos", "sin")] + [({f: 4097}, 3) for f in ("positions", "slots")])
+def test_rope_refusals(kw, want):
+    L = cq.lib()
+    assert L.cq_rope_append(ref(cache()), ref(rope(**kw)), None) == want
+
+
+@pytest.mark.parametrize("kw,want", BAD_CACHES)
+def test_cache_refusals(kw, want):
+    L = cq.lib()
+    assert L.cq_rope_append(ref(cache(**kw)), ref(rope()), None) == want
+    assert L.cq_attn_paged(ref(cache(**kw)), ref(attn()), OK, 1 << 40, None) == want
+    assert L.cq_attn_workspace_bytes(ref(cache(**kw)), ref(attn())) == -1
+
+
+def attn(**kw):
+    a = dict(q=OK, out=OK, q_stride=512, tokens=7, heads=4, batch=3, q_starts=OK, tables=OK, table_width=9, max_q=4,
+             max_kv=100, kv_lens=OK, scale=0.1, softcap=0.0, window=0, slopes=None, bidir=None, prefix_table=None,
+             prefix_len=0)
+    a.update(kw)
+    return cq_attn_args(**a)
+
+
+BAD_ATTN = [
+    (dict(q=None), 1), (dict(out=None), 1), (dict(kv_lens=None), 1), (dict(tables=None), 1), (dict(tokens=0), 1),
+    (dict(batch=0), 1), (dict(heads=0), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1), (dict(scale=float("inf")), 1),
+    (dict(scale=float("nan")), 1), (dict(softcap=-1.0), 1), (dict(softcap=float("nan")), 1), (dict(max_q=0), 1),
+    (dict(max_kv=-1), 1), (dict(table_width=-1), 1), (dict(heads=5), 2), (dict(q_stride=248), 2),
+    (dict(q_stride=260), 2), (dict(q_stride=1 << 41), 2), (dict(tokens=1 << 31), 2), (dict(q_starts=None), 2),
+    (dict(q_starts=None, tokens=3), 2), (dict(max_q=8), 2), (dict(max_kv=(1 << 30) + 1), 2),
+    (dict(table_width=1 << 30), 2), (dict(q=BAD), 3), (dict(out=BAD), 3), (dict(q_starts=4097), 3),
+    (dict(tables=4097), 3), (dict(kv_lens=4097), 3),
+]
+
+
+@pytest.mark.parametrize("kw,want", BAD_ATTN + [(dict(window=-1), 1), (dict(slopes=4097), 3), (dict(bidir=4097), 3)])
+def test_attn_refusals(kw, want):
+    L = cq.lib()
+    assert L.cq_attn_paged(ref(cache()), ref(attn(**kw)), OK, 1 << 40, None) == want
+    assert L.cq_attn_workspace_bytes(ref(cache()), ref(attn(**kw))) == -1
+
+
+@pytest.mark.parametrize("kw,want", BAD_ATTN + [
+    (dict(prefix_table=None), 1), (dict(prefix_len=-1), 1), (dict(prefix_len=(1 << 30) + 1), 2),
+    (dict(prefix_table=4097), 3), (dict(window=5), 8), (dict(slopes=OK), 8), (dict(bidir=OK), 8)])
+def test_shared_prefix_refusals(kw, want):
+    L = cq.lib()
+    a = attn(**{**dict(prefix_table=OK, prefix_len=40), **kw})
+    assert L.cq_attn_shared_prefix(ref(cache()), ref(a), OK, 1 << 40, None) == want
+    assert L.cq_attn_shared_prefix(ref(cache()), None, OK, 1 << 40, None) == 1
+
+
+def test_paged_call_takes_no_prefix():
+    L = cq.lib()
+    assert L.cq_attn_paged(ref(cache()), ref(attn(prefix_table=OK, prefix_len=4)), OK, 1 << 40, None) == 1
+    assert L.cq_attn_paged(None, ref(attn()), OK, 1 << 40, None) == 1
+
+
+def test_workspace_refusals():
+    L = cq.lib()
+    a = attn(max_kv=100000, table_width=6250, tokens=3, max_q=1)
+    need = L.cq_attn_workspace_bytes(ref(cache()), ref(a))
+    assert need >= 0
+    if need:
+        assert L.cq_attn_paged(ref(cache()), ref(a), None, 0, None) == 1
+        assert L.cq_attn_paged(ref(cache()), ref(a), OK, need - 1, None) == 2
+        assert L.cq_attn_paged(ref(cache()), ref(a), OK + 8, need, None) == 3
+
+
+def test_binding_refuses_shapes_and_types():
+    import torch
+    r, w = torch.zeros((3, 64)), torch.zeros((64,), dtype=torch.bfloat16)
+    with pytest.raises(AssertionError):
+        cq.cq_norm_residual(r, w[:32], 1e-5)
+    with pytest.raises(AssertionError):
+        cq.cq_norm_residual(r, w, 1e-5, y=r)  # y in another type than the weight
+    with pytest.raises(AssertionError):
+        cq.cq_norm_residual(r, w, 1e-5, gate=w)  # a gate of nothing
+    kv = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    q, one = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3,), dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        cq.cq_attn_paged(q, kv, kv, one.view(3, 1).long(), one, 5)
+    with pytest.raises(AssertionError):
+        cq.cq_attn_paged(q.half(), kv, kv, one.view(3, 1), one, 5)
+    with pytest.raises(AssertionError):
+        cq.cq_attn_paged(q.transpose(0, 1), kv, kv, one.view(3, 1), one, 5)
+    with pytest.raises(AssertionError):
+        cq.cq_rope_append(q, q, q, None, None, None, one, kv, kv)

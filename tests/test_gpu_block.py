@@ -1,0 +1,570 @@
+"""GPU: the operators between the packed products against plain 64-bit forms.
+
+Tolerances.  u is the unit roundoff of the output's type (2^-8 BF16, 2^-11
+FP16): the one rounding of an output costs u |y|.  FP32 sums of up to a few ten
+thousand terms and the hardware's exp and rsqrt stay within 2^-15 relative; a
+score of magnitude s adds s 2^-22 to the weight, below 2^-15 for the scores here.
+Attention may round its weights to the cache's type, u of sum(p |v|) more.
+"""
+import numpy as np
+import pytest
+
+from tests._cases import say
+
+pytestmark = pytest.mark.gpu
+
+U = {"bf16": 2.0**-8, "fp16": 2.0**-11}
+FP32 = 2.0**-15
+TINY = 2.0**-24  # smallest subnormal of FP16
+
+
+@pytest.fixture(scope="module")
+def torch_dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a visible MI355X"
+    import paper_2608_06763_amd as cq
+    cq.lib()
+    return torch
+
+
+def _cq():
+    import paper_2608_06763_amd as cq
+    return cq
+
+
+def _dtype(torch, name):
+    return torch.bfloat16 if name == "bf16" else torch.float16
+
+
+def _rand(torch, seed, *shape, dtype, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).to(_dtype(torch, dtype)).cuda()
+
+
+def _f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _within(got, ref, bound, what):
+    got = _f64(got)
+    assert got.shape == ref.shape
+    assert np.isfinite(got).all(), what
+    off = np.abs(got - ref) - bound
+    assert (off <= 0).all(), f"{what}: {np.max(off)} over the bound at {np.unravel_index(np.argmax(off), off.shape)}"
+
+
+# ---------------------------------------------------------------- norms
+
+
+def _norm_ref(r, w, eps, off, y, wp, gate, alpha):
+    if y is None:
+        total, mag = r, np.abs(r)
+    else:
+        u = y
+        if wp is not None:
+            u = u / np.sqrt((u * u).mean(1, keepdims=True) + eps) * (wp + off)
+        if gate is not None:
+            u = u * gate
+        total, mag = r + alpha * u, np.abs(r) + np.abs(alpha * u)
+    h = total / np.sqrt((total * total).mean(1, keepdims=True) + eps) * (w + off)
+    slack = mag / np.sqrt((total * total).mean(1, keepdims=True) + eps) * np.abs(w + off)
+    return h, total, mag, slack
+
+
+NORM_FORMS = [
+    dict(), dict(y=True), dict(y=True, post=True, off=1.0), dict(y=True, gate="row", alpha=-0.25),
+    dict(y=True, gate="all", post=True, r32=True), dict(y=True, r32=True, inplace=True, alpha=0.5),
+    dict(y=True, gate="strided", post=True, inplace=True),
+]
+
+
+@pytest.mark.parametrize("rows,width", [(1, 8), (3, 504), (5, 1024), (2, 2040), (1, 4096), (130, 4104), (600, 2056),
+                                        (2, 8192), (520, 8192), (3, 16384), (2, 32768)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_norm_residual(torch_dev, rows, width, dtype):
+    torch, cq = torch_dev, _cq()
+    for n, f in enumerate(NORM_FORMS):
+        say("norm", rows, width, dtype, f)
+        r = _rand(torch, 10 + n, rows, width, dtype=dtype, scale=3.0)
+        if f.get("r32"):
+            r = r.float() * 1.2345
+        w = _rand(torch, 20 + n, width, dtype=dtype)
+        y = _rand(torch, 30 + n, rows, width, dtype=dtype) if f.get("y") else None
+        wp = _rand(torch, 40 + n, width, dtype=dtype) if f.get("post") else None
+        gate = None
+        if f.get("gate") == "row":
+            gate = _rand(torch, 50 + n, rows, width, dtype=dtype)
+        elif f.get("gate") == "strided":
+            gate = _rand(torch, 50 + n, rows, width + 16, dtype=dtype)[:, 8:8 + width]
+        elif f.get("gate"):
+            gate = _rand(torch, 50 + n, width, dtype=dtype)
+        alpha, off = f.get("alpha", 1.0), f.get("off", 0.0)
+        opt = [None if t is None else _f64(t) for t in (y, wp, gate)]
+        h_ref, r_ref, mag, slack = _norm_ref(_f64(r), _f64(w), 1e-5, off, *opt, alpha)
+        h, r_out = cq.cq_norm_residual(r, w, 1e-5, y=y, post_weight=wp, gate=gate, alpha=alpha, weight_offset=off,
+                                       out=y if f.get("inplace") else None,
+                                       residual_out=r if f.get("inplace") else None)
+        _within(h, h_ref, U[dtype] * np.abs(h_ref) + FP32 * slack + TINY, "h")
+        ur = 2.0**-24 if f.get("r32") else U[dtype]
+        if y is None:
+            assert r_out is r
+        else:
+            _within(r_out, r_ref, ur * np.abs(r_ref) + FP32 * mag + TINY, "residual")
+
+
+def test_norm_of_zero_rows_and_not_a_number(torch_dev):
+    torch, cq = torch_dev, _cq()
+    r = torch.zeros((4, 256), dtype=torch.bfloat16, device="cuda")
+    r[1] = 3.0
+    r[2, 7] = float("nan")
+    w = torch.ones((256,), dtype=torch.bfloat16, device="cuda")
+    h, _ = cq.cq_norm_residual(r, w, 1e-6)
+    assert bool((h[0] == 0).all()) and bool((h[3] == 0).all()) and bool((h[1] == 1).all())
+    assert bool(torch.isnan(h[2]).all())
+
+
+@pytest.mark.parametrize("rows,width", [(1, 4096), (7, 96), (3, 1056), (70, 8192), (600, 2048), (600, 8192), (2, 14336)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_norm_to_carriers_equals_the_two_calls(torch_dev, rows, width, dtype):
+    torch, cq = torch_dev, _cq()
+    say("norm a8", rows, width, dtype)
+    r, y = (_rand(torch, 60 + i, rows, width, dtype=dtype, scale=2.0) for i in range(2))
+    w, wp = (_rand(torch, 70 + i, width, dtype=dtype) for i in range(2))
+    h, r_out = cq.cq_norm_residual(r, w, 1e-5, y=y, post_weight=wp)
+    x8_ref, dx_ref = cq.cq_quantize_act_a8(h)
+    out = torch.empty_like(h)
+    x8, dx, r8 = cq.cq_norm_residual_a8(r, w, 1e-5, y=y, post_weight=wp, out=out)
+    assert torch.equal(x8, x8_ref) and torch.equal(dx, dx_ref) and torch.equal(out, h) and torch.equal(r8, r_out)
+    x8, dx, _ = cq.cq_norm_residual_a8(r, w, 1e-5, y=y, post_weight=wp)
+    assert torch.equal(x8, x8_ref) and torch.equal(dx, dx_ref)
+
+
+# ---------------------------------------------------------------- rotation and append
+
+
+def _turn(x, cos, sin, interleaved):
+    """Rotated x and the sum of the magnitudes that make each channel."""
+    rot = 2 * cos.shape[1]
+    out, mag = x.copy(), np.abs(x)
+    lo, hi = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    c, s, a, b = cos[:, None], sin[:, None], x[..., lo], x[..., hi]
+    out[..., lo], out[..., hi] = a * c - b * s, b * c + a * s
+    mag[..., lo], mag[..., hi] = np.abs(a * c) + np.abs(b * s), np.abs(b * c) + np.abs(a * s)
+    return out, mag
+
+
+@pytest.mark.parametrize("dim,rot,interleaved", [(64, 64, False), (64, 16, False), (128, 128, False), (128, 96, True),
+                                                 (256, 256, True), (256, 64, False), (128, 0, False)])
+@pytest.mark.parametrize("tokens,heads,kv_heads,page,dtype", [(1, 4, 1, 16, "bf16"), (37, 6, 3, 32, "fp16"),
+                                                              (300, 35, 5, 128, "bf16")])
+def test_rope_append(torch_dev, dim, rot, interleaved, tokens, heads, kv_heads, page, dtype):
+    torch, cq = torch_dev, _cq()
+    say("append", dim, rot, interleaved, tokens, heads, kv_heads, page, dtype)
+    g = torch.Generator().manual_seed(3)
+    pages, rows = tokens // page + 3, 500
+    qkv = _rand(torch, 80, tokens, heads + 2 * kv_heads, dim, dtype=dtype)
+    q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+    angle = torch.randn((rows, rot // 2), generator=g).cuda()
+    cos, sin = (angle.cos(), angle.sin()) if rot else (None, None)
+    positions = torch.randint(0, rows, (tokens,), generator=g).to(torch.int32)
+    slots = torch.randperm(pages * page, generator=g)[:tokens].to(torch.int32)
+    if tokens > 2:
+        slots[1], slots[2] = -1, pages * page  # not appended
+    caches = [_rand(torch, 90 + i, pages, kv_heads, page, dim, dtype=dtype) for i in range(2)]
+    before = [_f64(c) for c in caches]
+    q_out = cq.cq_rope_append(q, k, v, cos, sin, positions.cuda(), slots.cuda(), *caches, interleaved=interleaved)
+    at = positions.numpy()
+    cn, sn = (_f64(cos)[at], _f64(sin)[at]) if rot else (np.zeros((tokens, 0)), np.zeros((tokens, 0)))
+    for got, x in ((q_out, q), (None, k)):
+        ref, mag = _turn(_f64(x), cn, sn, interleaved)
+        bound = U[dtype] * np.abs(ref) + 2.0**-22 * mag + TINY
+        if got is not None:
+            _within(got, ref, bound, "q")
+            continue
+        k_ref, k_bound = before[0].copy(), np.zeros_like(before[0])
+        v_ref = before[1].copy()
+        for i, s in enumerate(slots.tolist()):
+            if 0 <= s < pages * page:
+                k_ref[s // page, :, s % page], k_bound[s // page, :, s % page] = ref[i], bound[i]
+                v_ref[s // page, :, s % page] = _f64(v)[i]
+        _within(caches[0], k_ref, k_bound, "k")  # untouched slots: exactly
+        assert np.array_equal(_f64(caches[1]), v_ref)
+    # in place, on the fused product
+    same = cq.cq_rope_append(q, k, v, cos, sin, positions.cuda(), slots.cuda(), *caches, interleaved=interleaved,
+                             q_out=q)
+    assert same is q and torch.equal(q, q_out)
+
+
+def test_rope_positions_outside_the_tables_are_clamped(torch_dev):
+    torch, cq = torch_dev, _cq()
+    q, kv = _rand(torch, 1, 3, 2, 64, dtype="bf16"), _rand(torch, 2, 3, 1, 64, dtype="bf16")
+    angle = torch.arange(5 * 32, device="cuda").view(5, 32).float()
+    slots = torch.arange(3, device="cuda", dtype=torch.int32)
+
+    def go(p):
+        caches = [torch.zeros((1, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        pos = torch.tensor(p, device="cuda", dtype=torch.int32)
+        return cq.cq_rope_append(q, kv, kv, angle.cos(), angle.sin(), pos, slots, *caches)
+
+    assert torch.equal(go([-7, 5, 1 << 30]), go([0, 4, 4]))
+
+
+# ---------------------------------------------------------------- attention
+
+
+def _paged(torch, seed, lens, page, kv_heads, dim, dtype, spare=3, garbage=float("nan")):
+    """Caches whose pages lie in random order, with `garbage` wherever no token is
+    held, and tables with wild entries past each sequence's end; and the keys and
+    values of every sequence."""
+    g = torch.Generator().manual_seed(seed)
+    need = [-(-n // page) for n in lens]
+    pages, width = sum(need) + spare, max(max(need), 1) + 1
+    order = torch.randperm(pages, generator=g)
+    pools = [torch.full((pages, kv_heads, page, dim), garbage) for _ in range(2)]
+    tables = torch.full((len(lens), width), -5, dtype=torch.int32)
+    tables[:, -1] = 1 << 30
+    held, at = [], 0
+    for b, n in enumerate(lens):
+        own = order[at:at + need[b]]
+        at += need[b]
+        tables[b, :need[b]] = own.to(torch.int32)
+        kv = []
+        for i, pool in enumerate(pools):
+            x = torch.randn((n, kv_heads, dim), generator=g) + (0.2 if i else 0.0)
+            x = x.to(_dtype(torch, dtype)).float()
+            for p in range(need[b]):
+                part = x[p * page:(p + 1) * page]
+                pool[own[p], :, :part.shape[0]] = part.transpose(0, 1)
+            kv.append(x.double().numpy())
+        held.append(kv)
+    return [p.to(_dtype(torch, dtype)).cuda() for p in pools], tables.cuda(), held
+
+
+def _attn_ref(q, held, new, scale, softcap=0.0, window=0, slopes=None, bidir=None, prefix=None):
+    """Outputs, and sum(p |v|), per row of q [tokens, heads, dim]."""
+    tokens, heads, dim = q.shape
+    out, mag, row = np.zeros_like(q), np.zeros_like(q), 0
+    for b, n in enumerate(new):
+        k, v = held[b]
+        length, group = k.shape[0], heads // k.shape[1]
+        i = np.arange(length - n, length)[:, None]
+        j = np.arange(length)[None]
+        seen = j <= i
+        if window:
+            seen &= j > i - window
+        if bidir is not None:
+            seen |= (j < bidir[b]) & (i >= 0)
+        for h in range(heads):
+            s = q[row:row + n, h] @ k[:, h // group].T * scale
+            if softcap:
+                s = softcap * np.tanh(s / softcap)
+            if slopes is not None:
+                s = s + slopes[h] * (j - i)
+            s = np.where(seen, s, -np.inf)
+            vv = v[:, h // group]
+            if prefix is not None:
+                f = q[row:row + n, h] @ prefix[0][:, h // group].T * scale
+                if softcap:
+                    f = softcap * np.tanh(f / softcap)
+                s, vv = np.concatenate((f, s), 1), np.concatenate((prefix[1][:, h // group], vv))
+            if n == 0 or s.shape[1] == 0:
+                continue
+            top = s.max(1, keepdims=True)
+            p = np.exp(s - np.where(np.isinf(top), 0.0, top))
+            p = p / np.where(p.sum(1, keepdims=True) > 0, p.sum(1, keepdims=True), 1.0)
+            # hidden tokens do not reach the output, whatever they hold
+            used = np.where(p.max(0) > 0, 1.0, 0.0)[:, None]
+            vv = np.where(used > 0, vv, 0.0)
+            out[row:row + n, h], mag[row:row + n, h] = p @ vv, p @ np.abs(vv)
+        row += n
+    return out, mag
+
+
+def _check_attn(torch, dtype, dim, heads, kv_heads, page, new, lens, seed=5, max_kv=None, starts=None, garbage=np.nan,
+                **opt):
+    cq = _cq()
+    say("attn", dtype, dim, heads, kv_heads, page, new, lens, {k: v for k, v in opt.items() if k != "slopes"})
+    caches, tables, held = _paged(torch, seed, lens, page, kv_heads, dim, dtype, garbage=garbage)
+    total = sum(new)
+    qkv = _rand(torch, seed + 1, total, heads + 2 * kv_heads, dim, dtype=dtype, scale=1.5)
+    q = qkv[:, :heads]
+    if starts is None and max(new) > 1 or min(new) != 1:
+        starts = torch.tensor(np.cumsum([0] + new), dtype=torch.int32).cuda()
+    args = dict(opt)
+    for name, kind in (("slopes", torch.float32), ("bidir", torch.int32)):
+        if args.get(name) is not None:
+            args[name] = torch.tensor(args[name], dtype=kind).cuda()
+    out = cq.cq_attn_paged(q, *caches, tables, torch.tensor(lens, dtype=torch.int32).cuda(),
+                           max(max(lens), 0) if max_kv is None else max_kv, q_starts=starts, max_q=max(new), **args)
+    ref, mag = _attn_ref(_f64(q), held, new, opt.pop("scale", dim**-0.5), **opt)
+    u = U[dtype]
+    _within(out, ref, u * np.abs(ref) + (u + FP32) * mag + TINY, "attention")
+    return out
+
+
+# lengths on both sides of the edges of pages and of tiles of 16, 32, 64, 128
+LENS = [1, 15, 16, 17, 31, 32, 33, 64, 65, 127, 129, 300]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 2), (7, 1), (20, 4), (33, 1), (16, 16)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_attn_single_tokens(torch_dev, dtype, dim, heads, kv_heads, page):
+    _check_attn(torch_dev, dtype, dim, heads, kv_heads, page, [1] * len(LENS), LENS)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads,page", [(2, 2, 16), (8, 2, 32), (5, 1, 128)])
+@pytest.mark.parametrize("new,lens", [
+    ([1, 2, 3, 7, 8, 4], [1, 2, 30, 64, 65, 400]),          # a few tokens each
+    ([5, 33, 64, 17, 1], [5, 33, 64, 17, 1]),               # prompts
+    ([130, 257, 63], [130, 300, 190]),                      # prompts and chunks
+    ([0, 3, 0, 1, 0], [40, 3, 0, 9, 7]),                    # sequences without queries
+])
+def test_attn_ragged(torch_dev, dtype, dim, heads, kv_heads, page, new, lens):
+    _check_attn(torch_dev, dtype, dim, heads, kv_heads, page, new, lens)
+
+
+OPTIONS = [dict(softcap=5.0), dict(window=1), dict(window=20), dict(window=100), dict(scale=0.31),
+           dict(slopes=[0.5, 0.01, 0.25, 1.0]), dict(softcap=8.0, window=50, slopes=[0.1, 0.3, 0.0, 2.0]),
+           dict(bidir=[0, 7, 500, 33, 1]), dict(bidir=[90, 0, 64, 5, 1], window=16, softcap=20.0)]
+
+
+@pytest.mark.parametrize("opt", OPTIONS, ids=str)
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("bf16", 256)])
+@pytest.mark.parametrize("new,lens", [([1, 1, 1, 1, 1], [1, 40, 129, 33, 290]), ([4, 6, 2, 1, 5], [4, 70, 129, 40, 33]),
+                                      ([90, 200, 64, 33, 140], [90, 230, 64, 300, 140])])
+def test_attn_scores_and_masks(torch_dev, opt, dtype, dim, new, lens):
+    _check_attn(torch_dev, dtype, dim, 4, 2, 16, new, lens, **opt)
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1, 1], [0, 1, 0]), ([3, 5, 2], [0, 2, 9]), ([100, 150], [20, 0]),
+                                      ([1], [0])])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("fp16", 256)])
+def test_attn_rows_that_see_nothing_are_zero(torch_dev, dtype, dim, new, lens):
+    out = _check_attn(torch_dev, dtype, dim, 4, 2, 16, new, lens, bidir=[4] * len(new))
+    row = 0
+    for n, length in zip(new, lens):
+        assert bool((out[row:row + max(0, n - length)] == 0).all())
+        row += n
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new", [3, 40, 150])
+def test_attn_hidden_tokens_may_hold_anything(torch_dev, dtype, dim, bad, new):
+    # the last token's value (and key, if no number) is bad: all queries but the
+    # last are as before, up to the rounding of outputs and weights on either side
+    # (2 u of a mean magnitude below 2)
+    torch, cq = torch_dev, _cq()
+    say("attn hidden", dtype, dim, bad, new)
+    heads, kv_heads, page, length = 4, 2, 16, new + 21
+    caches, tables, held = _paged(torch, 9, [length], page, kv_heads, dim, dtype, garbage=bad)
+    q = _rand(torch, 10, new, heads, dim, dtype=dtype)
+    starts = torch.tensor([0, new], dtype=torch.int32).cuda()
+    lens = torch.tensor([length], dtype=torch.int32).cuda()
+    good = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new)
+    at = int(tables[0, (length - 1) // page])
+    caches[1][at, :, (length - 1) % page] = bad
+    if bad != bad:
+        caches[0][at, 0, (length - 1) % page, 1] = bad
+    out = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new)
+    near = dict(rtol=2 * U[dtype], atol=4 * U[dtype])
+    assert torch.allclose(out[:-1].float(), good[:-1].float(), **near)
+    assert not bool(torch.isfinite(out[-1]).any())
+    # and one that the window has left behind
+    caches[1][at, :, (length - 1) % page] = 1.0
+    caches[0][at, 0, (length - 1) % page, 1] = 1.0
+    base = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new, window=5)
+    caches[1][int(tables[0, 0]), :, 3] = bad
+    caches[1][int(tables[0, 1]), :, 1] = bad  # token 17: the first query (21) just sees it
+    out = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new, window=5)
+    assert torch.allclose(out[1:].float(), base[1:].float(), **near) and not bool(torch.isfinite(out[0]).any())
+
+
+def test_attn_long_history(torch_dev):
+    _check_attn(torch_dev, "bf16", 128, 8, 2, 64, [1], [5003])
+    _check_attn(torch_dev, "fp16", 64, 4, 2, 16, [1, 2, 1], [4000, 9, 1700])
+    _check_attn(torch_dev, "fp16", 64, 4, 1, 128, [70, 2], [4000, 3])
+
+
+def test_attn_many_sequences(torch_dev):
+    rng = np.random.default_rng(4)
+    lens = [int(n) for n in rng.integers(0, 90, 700)]
+    _check_attn(torch_dev, "bf16", 64, 2, 1, 16, [1] * 700, lens)
+
+
+def test_attn_bounds_cut_the_sequences(torch_dev):
+    # lengths past max_kv, or past the table, are cut; nothing outside is read
+    torch, cq = torch_dev, _cq()
+    caches, tables, held = _paged(torch, 2, [64, 40], 16, 1, 64, "bf16")
+    q = _rand(torch, 3, 2, 2, 64, dtype="bf16")
+
+    def go(lens, max_kv, table):
+        return cq.cq_attn_paged(q, *caches, table.contiguous(), torch.tensor(lens, dtype=torch.int32).cuda(), max_kv)
+
+    want = go([40, 40], 40, tables)
+    assert torch.equal(go([2**31 - 1, 41], 40, tables), want)
+    assert torch.equal(go([48, -3], 1000, tables)[0], go([1000, -3], 1000, tables[:, :3])[0])
+    assert bool((go([48, -3], 1000, tables)[1] == 0).all())
+
+
+def test_attn_large_scores(torch_dev):
+    # one token far above the others, and equal scores of large magnitude
+    torch, cq = torch_dev, _cq()
+    for dtype in ("bf16", "fp16"):
+        caches, tables, held = _paged(torch, 6, [150, 150], 16, 1, 64, dtype)
+        for c, table in ((caches[0], tables),):
+            c[int(table[0, 2]), 0, 5] = 30.0
+            c[table[1, :10].long()] = -60.0
+        held[0][0][37, 0] = 30.0
+        held[1][0][:] = -60.0
+        q = torch.full((2, 2, 64), 10.0, dtype=_dtype(torch, dtype), device="cuda")
+        out = cq.cq_attn_paged(q, *caches, tables, torch.tensor([150, 150], dtype=torch.int32).cuda(), 150)
+        ref, mag = _attn_ref(_f64(q), held, [1, 1], 0.125)
+        _within(out, ref, U[dtype] * np.abs(ref) + (U[dtype] + FP32) * mag + TINY, "large scores")
+
+
+def test_attn_offsets_past_32_bits(torch_dev):
+    # pools of 6 GiB each; the sequence lies at their ends
+    torch, cq = torch_dev, _cq()
+    kv_heads, page, dim, length = 8, 64, 128, 700
+    pages = (6 << 30) // (kv_heads * page * dim * 2)
+    pools = [torch.empty((pages, kv_heads, page, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    n = -(-length // page)
+    own = torch.tensor([pages - 1 - 2 * i for i in range(n)])
+    x = [_rand(torch, 11 + i, n, kv_heads, page, dim, dtype="bf16") for i in range(2)]
+    for pool, part in zip(pools, x):
+        pool[own.cuda()] = part
+    held = [[_f64(t.transpose(1, 2).reshape(n * page, kv_heads, dim)[:length]) for t in x]]
+    table = own.to(torch.int32).view(1, n).cuda()
+    lens = torch.tensor([length], dtype=torch.int32).cuda()
+    for new in (1, 200):
+        q = _rand(torch, 13, new, 16, dim, dtype="bf16")
+        out = cq.cq_attn_paged(q, *pools, table, lens, length,
+                               q_starts=torch.tensor([0, new], dtype=torch.int32).cuda(), max_q=new)
+        ref, mag = _attn_ref(_f64(q), held, [new], dim**-0.5)
+        _within(out, ref, U["bf16"] * np.abs(ref) + (U["bf16"] + FP32) * mag + TINY, "far pages")
+    # and the append reaches them
+    qkv = _rand(torch, 14, 2, 16 + 2 * kv_heads, dim, dtype="bf16")
+    slots = torch.tensor([pages * page - 1, 5], dtype=torch.int32).cuda()
+    cq.cq_rope_append(qkv[:, :16], qkv[:, 16:24], qkv[:, 24:], None, None, None, slots, *pools)
+    assert torch.equal(pools[0][-1, :, -1], qkv[0, 16:24]) and torch.equal(pools[1][0, :, 5], qkv[1, 24:])
+
+
+# ---------------------------------------------------------------- shared prefix
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads,page", [(2, 2, 16), (8, 2, 32), (7, 1, 64)])
+@pytest.mark.parametrize("prefix,new,lens", [
+    (33, [1, 1, 1], [5, 0, 70]), (500, [1] * 20, list(range(0, 60, 3))), (1, [1], [1]), (0, [1, 1], [3, 40]),
+    (130, [3, 1, 40], [3, 20, 50]), (64, [1] * 150, [k % 37 for k in range(150)]),
+])
+def test_attn_shared_prefix(torch_dev, dtype, dim, heads, kv_heads, page, prefix, new, lens):
+    torch, cq = torch_dev, _cq()
+    say("shared", dtype, dim, heads, kv_heads, page, prefix, len(new))
+    caches, tables, held = _paged(torch, 21, [prefix] + lens, page, kv_heads, dim, dtype)
+    q = _rand(torch, 22, sum(new), heads + 2 * kv_heads, dim, dtype=dtype, scale=1.5)[:, :heads]
+    starts = None
+    if max(new) > 1:
+        starts = torch.tensor(np.cumsum([0] + new), dtype=torch.int32).cuda()
+    for opt in (dict(), dict(softcap=4.0, scale=0.2)):
+        out = cq.cq_attn_shared_prefix(q, *caches, tables[0].contiguous(), prefix, tables[1:].contiguous(),
+                                       torch.tensor(lens, dtype=torch.int32).cuda(), max(lens), q_starts=starts,
+                                       max_q=max(new), **opt)
+        ref, mag = _attn_ref(_f64(q), held[1:], new, opt.get("scale", dim**-0.5), softcap=opt.get("softcap", 0.0),
+                             prefix=held[0])
+        u = U[dtype]
+        _within(out, ref, u * np.abs(ref) + (u + FP32) * mag + TINY, "shared prefix")
+
+
+def test_attn_shared_prefix_without_own_tokens(torch_dev):
+    torch, cq = torch_dev, _cq()
+    caches, tables, held = _paged(torch, 23, [90], 16, 2, 64, "bf16")
+    q = _rand(torch, 24, 6, 4, 64, dtype="bf16")
+    lens = torch.zeros((6,), dtype=torch.int32, device="cuda")
+    none = torch.empty((6, 0), dtype=torch.int32, device="cuda")
+    out = cq.cq_attn_shared_prefix(q, *caches, tables[0].contiguous(), 90, none, lens, 0)
+    empty = [[np.zeros((0, 2, 64))] * 2] * 6
+    ref, mag = _attn_ref(_f64(q), empty, [1] * 6, 0.125, prefix=held[0])
+    _within(out, ref, U["bf16"] * np.abs(ref) + (U["bf16"] + FP32) * mag + TINY, "prefix alone")
+
+
+# ---------------------------------------------------------------- streams, graphs, repeats
+
+
+def _block(torch, seed):
+    """Inputs of a norm, an append and an attention over what was appended."""
+    heads, kv_heads, dim, page, batch = 8, 2, 64, 16, 5
+    caches, tables, held = _paged(torch, seed, [60, 9, 200, 33, 1], page, kv_heads, dim, "bf16")
+    lens = torch.tensor([60, 9, 200, 33, 1], dtype=torch.int32).cuda()
+    last = (lens - 1).long()
+    slots = (tables[torch.arange(batch).cuda(), last // page].long() * page + last % page).to(torch.int32)
+    qkv = _rand(torch, seed + 1, batch, heads + 2 * kv_heads, dim, dtype="bf16")
+    angle = torch.arange(256 * 32, device="cuda").view(256, 32) * 0.01
+    x = _rand(torch, seed + 2, batch, heads * dim, dtype="bf16")
+    w = _rand(torch, seed + 3, heads * dim, dtype="bf16")
+    return caches, tables, lens, slots, qkv, angle.cos(), angle.sin(), x, w
+
+
+def _run_block(cq, inputs, stream=None):
+    caches, tables, lens, slots, qkv, cos, sin, x, w = inputs
+    q = cq.cq_rope_append(qkv[:, :8], qkv[:, 8:10], qkv[:, 10:], cos, sin, (lens - 1), slots, *caches, stream=stream)
+    o = cq.cq_attn_paged(q, *caches, tables, lens, 200, stream=stream)
+    s = cq.cq_attn_shared_prefix(q, *caches, tables[2].contiguous(), 150, tables, lens, 200, stream=stream)
+    h, r = cq.cq_norm_residual(x, w, 1e-5, y=o.view(o.shape[0], -1), post_weight=w, stream=stream)
+    return o, s, h, r
+
+
+def test_block_repeats_bit_for_bit_and_on_another_stream(torch_dev):
+    torch, cq = torch_dev, _cq()
+    inputs = _block(torch, 31)
+    first = [t.clone() for t in _run_block(cq, inputs)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        other = _run_block(cq, inputs)
+    side.synchronize()
+    for a, b, c in zip(first, other, _run_block(cq, inputs)):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_block_in_a_graph(torch_dev):
+    torch, cq = torch_dev, _cq()
+    inputs = _block(torch, 41)
+    _run_block(cq, inputs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = _run_block(cq, inputs)
+    for seed in (51, 52, 53):
+        fresh = _block(torch, seed)
+        for i in (4, 7):
+            inputs[i].copy_(fresh[i])
+        want = [t.clone() for t in _run_block(cq, inputs)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
+def test_attn_workspace_of_the_caller(torch_dev):
+    torch, cq = torch_dev, _cq()
+    caches, tables, held = _paged(torch, 61, [3000, 10], 16, 2, 128, "bf16")
+    q = _rand(torch, 62, 2, 8, 128, dtype="bf16")
+    lens = torch.tensor([3000, 10], dtype=torch.int32).cuda()
+    need = cq.cq_attn_workspace_bytes(q, *caches, tables, lens, 3000)
+    want = cq.cq_attn_paged(q, *caches, tables, lens, 3000)
+    # whatever the workspace holds, the result is the same
+    ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(cq.cq_attn_paged(q, *caches, tables, lens, 3000, workspace=ws), want)
+    if need > 0:
+        with pytest.raises(cq.CQError) as e:
+            cq.cq_attn_paged(q, *caches, tables, lens, 3000, workspace=ws[:need - 16])
+        assert e.value.status == 2

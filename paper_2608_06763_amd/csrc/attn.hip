@@ -1,84 +1,135 @@
-// Attention over a paged cache: one wave for each query and head, one token of
-// the cache at a time, with the running maximum and sum of the softmax.
-#include "block_internal.h"
-#include "cq_device.h"
-#include "stream_common.h"
+// Attention over a paged cache: which kernels a call runs, and where its parts
+// lie in the workspace.
+#include "attn_common.h"
 
 namespace cq {
 
 namespace {
 
-template <int DT, int D>
-__global__ void __launch_bounds__(256) attn_kernel(cq_kv_cache c, cq_attn_args a) {
-    constexpr int E = D / kWave;
-    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= a.tokens * a.heads) return;
-    const int64_t token = row / a.heads;
-    const int head = int(row % a.heads), group = a.heads / c.kv_heads, kvh = head / group;
-    int b = int(token), first = int(token), n = 1;
-    if (a.q_starts) {
-        int lo = 0, hi = a.batch - 1;  // last b with q_starts[b] <= token
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (a.q_starts[mid] <= token) lo = mid; else hi = mid - 1;
-        }
-        b = lo;
-        first = a.q_starts[b];
-        n = a.q_starts[b + 1] - first;
-    }
-    const int64_t held = min(int64_t(a.max_kv), int64_t(a.table_width) * c.page);
-    const int len = int(min(int64_t(max(a.kv_lens[b], 0)), held));
-    const int pos = len - n + int(token) - first;
-    const int bidir = a.bidir ? a.bidir[b] : 0;
-    const float slope = a.slopes ? a.slopes[head] : 0.f;
-    float q[E], o[E], m = -3e38f, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        q[e] = act_to_f32<DT>(static_cast<const uint16_t *>(a.q)[token * a.q_stride + int64_t(head) * D + e * 64 + lane]);
-        o[e] = 0.f;
-    }
-    auto visit = [&](const int32_t *table, int j, float bias) {
-        const int64_t page = min(uint64_t(uint32_t(table[j / c.page])), uint64_t(c.pages - 1));
-        const int64_t at = ((page * c.kv_heads + kvh) * c.page + j % c.page) * D;
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s += q[e] * act_to_f32<DT>(static_cast<const uint16_t *>(c.k)[at + e * 64 + lane]);
-        s = wave_sum(s) * a.scale;
-        if (a.softcap > 0.f) s = a.softcap * tanhf(s / a.softcap);
-        s += bias;
-        const float top = fmaxf(m, s), keep = __expf(m - top), p = __expf(s - top);
-        m = top;
-        l = l * keep + p;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            o[e] = o[e] * keep + p * act_to_f32<DT>(static_cast<const uint16_t *>(c.v)[at + e * 64 + lane]);
-    };
-    for (int j = 0; j < int(a.prefix_len); ++j) visit(a.prefix_table, j, 0.f);
-    for (int j = 0; j < len; ++j) {
-        const bool seen = (j <= pos && (a.window == 0 || j > pos - a.window)) || (j < bidir && pos >= 0);
-        if (seen) visit(a.tables + int64_t(b) * a.table_width, j, slope * float(j - pos));
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        store_out<DT>(a.out, (token * a.heads + head) * D + e * 64 + lane, l == 0.f ? 0.f : o[e] / l);
+// The rows kernel for `sequences` of at most `rows` rows and `tokens` tokens.
+rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t tokens, bool keep) {
+    rows_plan r;
+    r.nt = rows <= 16 ? 1 : rows <= 32 || dim == 256 ? 2 : 4;
+    r.row_tiles = int((rows + 16 * r.nt - 1) / (16 * r.nt));
+    r.numbers = sequences * kv_heads * r.row_tiles;
+    const int64_t units = tokens > 32 ? (tokens + 31) / 32 : 1;
+    r.min_units = 4;
+    r.split = units > 8;
+    // workgroups that LDS and registers let run at once
+    const int64_t most = int64_t(device_cu_count()) * (dim == 256 || r.nt == 4 ? 1 : 2);
+    const int64_t need = (r.numbers * units + r.min_units - 1) / r.min_units;
+    r.grid = int(r.split ? (need < most ? need : most) : r.numbers);
+    r.slots = (r.split ? 2 * int64_t(r.grid) : 0) + (keep ? r.numbers : 0);
+    return r;
 }
 
-template <int DT>
-hipError_t launch_dt(const cq_kv_cache &c, const cq_attn_args &a, hipStream_t stream) {
-    const dim3 grid(uint32_t((a.tokens * a.heads + 3) / 4)), block(256);
-    if (c.dim == 64) hipLaunchKernelGGL((attn_kernel<DT, 64>), grid, block, 0, stream, c, a);
-    else if (c.dim == 128) hipLaunchKernelGGL((attn_kernel<DT, 128>), grid, block, 0, stream, c, a);
-    else hipLaunchKernelGGL((attn_kernel<DT, 256>), grid, block, 0, stream, c, a);
-    return hipGetLastError();
+struct source_bytes {
+    int64_t o, ml, shares;
+    int64_t all() const { return o + ml + shares; }
+};
+source_bytes bytes_of(const rows_plan &r, int dim, bool keep) {
+    const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
+    if (!r.split && !keep) return {0, 0, 0};
+    const int64_t rows = r.slots * 16 * r.nt;
+    return {up(rows * dim * 4), up(rows * 8), up(r.numbers * int64_t(sizeof(int2)))};
+}
+
+// Points a launch's parts at `ws`, and the join at them.
+join_source place(attn_params &p, const rows_plan &r, const source_bytes &n, bool keep, uint8_t *ws) {
+    p.part_o = reinterpret_cast<float *>(ws);
+    p.part_ml = reinterpret_cast<float *>(ws + n.o);
+    p.shares = n.shares ? reinterpret_cast<int2 *>(ws + n.o + n.ml) : nullptr;
+    p.row_tiles = r.row_tiles;
+    p.min_units = r.min_units;
+    p.keep_parts = keep;
+    join_source j = {p.part_o, p.part_ml, p.shares, n.shares ? 16 * r.nt : 0, r.row_tiles, r.grid, 0, -1};
+    if (keep) j.first = r.split ? 2 * int64_t(r.grid) : 0;
+    return j;
+}
+
+hipError_t launch_rows(int dt, int dim, const rows_plan &r, const attn_params &p, hipStream_t stream) {
+    if (dt == 0) {
+        if (dim == 64) return attn_rows_bf16_64(r, p, stream);
+        return dim == 128 ? attn_rows_bf16_128(r, p, stream) : attn_rows_bf16_256(r, p, stream);
+    }
+    if (dim == 64) return attn_rows_fp16_64(r, p, stream);
+    return dim == 128 ? attn_rows_fp16_128(r, p, stream) : attn_rows_fp16_256(r, p, stream);
+}
+
+struct plan_t {
+    rows_plan own, flat;
+    source_bytes own_bytes, flat_bytes;
+    bool shared;
+    int64_t max_kv;
+};
+
+plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
+    plan_t t;
+    const int64_t group = a.heads / c.kv_heads, held = int64_t(a.table_width) * c.page;
+    t.max_kv = a.max_kv < held ? a.max_kv : held;
+    t.shared = a.prefix_len > 0;
+    t.own = plan_rows(c.dim, a.batch, c.kv_heads, a.max_q * group, t.max_kv, t.shared);
+    t.own_bytes = bytes_of(t.own, c.dim, t.shared);
+    t.flat_bytes = {0, 0, 0};
+    if (t.shared) {
+        t.flat = plan_rows(c.dim, 1, c.kv_heads, a.tokens * group, a.prefix_len, true);
+        t.flat_bytes = bytes_of(t.flat, c.dim, true);
+    }
+    return t;
 }
 
 }  // namespace
 
-int64_t attn_workspace_bytes(const cq_kv_cache &, const cq_attn_args &) { return 0; }
+int64_t attn_workspace_bytes(const cq_kv_cache &c, const cq_attn_args &a) {
+    const plan_t t = make_plan(c, a);
+    return t.own_bytes.all() + t.flat_bytes.all();
+}
 
-hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *, hipStream_t stream) {
-    return c.dtype == CQ_BF16 ? launch_dt<0>(c, a, stream) : launch_dt<1>(c, a, stream);
+hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *workspace, hipStream_t stream) {
+    const plan_t t = make_plan(c, a);
+    attn_params p = {};
+    p.q = static_cast<const uint16_t *>(a.q);
+    p.k = static_cast<const uint16_t *>(c.k);
+    p.v = static_cast<const uint16_t *>(c.v);
+    p.out = static_cast<uint16_t *>(a.out);
+    p.q_stride = a.q_stride;
+    p.tokens = a.tokens;
+    p.heads = a.heads;
+    p.kv_heads = c.kv_heads;
+    p.group = a.heads / c.kv_heads;
+    p.batch = a.batch;
+    p.q_starts = a.q_starts;
+    p.tables = a.tables;
+    p.kv_lens = a.kv_lens;
+    p.bidir = a.bidir;
+    p.slopes = a.slopes;
+    p.table_width = a.table_width;
+    p.max_kv = int(t.max_kv);
+    p.max_q = a.max_q;
+    p.page_shift = __builtin_ctz(unsigned(c.page));
+    p.pages = uint32_t(c.pages);
+    p.window = a.window;
+    p.scale = a.scale;
+    p.softcap = a.softcap;
+
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    join_source flat = {};
+    if (t.shared) {
+        attn_params f = p;
+        f.flat = 1;
+        f.flat_len = int(a.prefix_len);
+        f.tables = a.prefix_table;
+        f.kv_lens = f.bidir = nullptr;
+        f.q_starts = nullptr;
+        f.batch = 1;
+        flat = place(f, t.flat, t.flat_bytes, true, ws + t.own_bytes.all());
+        const hipError_t e = launch_rows(int(c.dtype), c.dim, t.flat, f, stream);
+        if (e != hipSuccess) return e;
+    }
+    const join_source own = place(p, t.own, t.own_bytes, t.shared, ws);
+    const hipError_t e = launch_rows(int(c.dtype), c.dim, t.own, p, stream);
+    if (e != hipSuccess || !own.rows) return e;
+    return launch_attn_join(int(c.dtype), c.dim, p, own, flat, stream);
 }
 
 }  // namespace cq

@@ -1,0 +1,311 @@
+// Building blocks of the attention kernels (gfx950).
+//
+// All of them form S^T = K Q^T and O^T = V^T P^T on the matrix cores.  The
+// product's result layout gives every lane one query (a column) and a few of its
+// scores, so the softmax of a query stays in a lane and its neighbours across the
+// 16- or 32-lane rows, and the weights leave the softmax in the very registers
+// that the second product takes as an operand: its tokens are summed in the order
+// in which the lanes hold them, which V^T's operand follows.  V^T is read from
+// the LDS tile of V with the transposing LDS read, which hands each lane four
+// tokens of one channel.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "block_internal.h"
+#include "cq_device.h"
+#include "wide_common.h"
+
+namespace cq {
+
+constexpr float kLog2e = 1.4426950408889634f;
+// The running maximum starts here and not at -inf, so that differences of two
+// maxima stay numbers.  A row that sees nothing keeps it, with a sum of 0.
+constexpr float kLowest = -3.0e38f;
+// The running maximum is only moved, and the sums rescaled, when a score passes
+// it by more than this many powers of two.
+constexpr float kSlack = 4.0f;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// What the kernels take, from validated arguments.  One launch covers the
+// sequences' own tokens, or (flat) one sequence of every query, each of which
+// sees all of its flat_len tokens: the shared prefix.
+struct attn_params {
+    const uint16_t *q, *k, *v;
+    uint16_t *out;
+    int64_t q_stride;
+    int64_t tokens;
+    int heads, kv_heads, group, batch;
+    const int32_t *q_starts, *tables, *kv_lens, *bidir;
+    const float *slopes;
+    int table_width, max_kv;  // max_kv: no more than the tables hold
+    int max_q;                // no sequence has more rows, whatever q_starts holds
+    int page_shift;
+    uint32_t pages;
+    int window;
+    float scale, softcap;
+    int flat, flat_len;
+    int row_tiles;     // most row tiles of a sequence
+    int min_units;     // least units of a workgroup (rows kernel)
+    int keep_parts;    // every part goes to the workspace
+    float *part_o;     // [slot][rows of a tile][dim], not normalised
+    float *part_ml;    // [slot][rows of a tile][2]: maximum (powers of two), sum
+    int2 *shares;      // [sequence][key head][row tile]: who holds its parts
+};
+
+// An index array that no kernel writes, at a wave-uniform index: a scalar load.
+__device__ __forceinline__ int32_t index_at(const int32_t *p, int64_t i) {
+    return reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
+struct seq_t {
+    int first, n, len;  // first query row, queries, tokens held
+};
+
+__device__ __forceinline__ seq_t sequence(const attn_params &p, int b) {
+    if (p.flat) return {0, int(p.tokens), p.flat_len};
+    seq_t s = {b, 1, 0};
+    if (p.q_starts) {
+        // whatever the array holds, the rows stay inside q
+        s.first = min(max(p.q_starts[b], 0), int(p.tokens));
+        s.n = min(min(max(p.q_starts[b + 1], s.first), int(p.tokens)) - s.first, p.max_q);
+    }
+    s.len = min(max(p.kv_lens[b], 0), p.max_kv);
+    return s;
+}
+
+// What one query sees: j < hi && j >= lo, or j < bi.
+struct limits_t {
+    int hi, lo, bi, pos;
+};
+
+__device__ __forceinline__ limits_t limits(const attn_params &p, const seq_t &s, int i, bool valid, int bidir) {
+    limits_t r = {0, 0, 0, 0};
+    if (!valid) return r;
+    if (p.flat) {
+        r.hi = s.len;
+        return r;
+    }
+    r.pos = s.len - s.n + i;
+    r.hi = r.pos + 1;
+    if (p.window) r.lo = r.pos - p.window + 1;
+    if (r.pos >= 0) r.bi = min(bidir, s.len);
+    return r;
+}
+
+__device__ __forceinline__ bool sees(const limits_t &r, int j) { return (j < r.hi && j >= r.lo) || j < r.bi; }
+
+// sequence() at a wave-uniform b.
+__device__ __forceinline__ seq_t sequence_uniform(const attn_params &p, int b) {
+    if (p.flat) return {0, int(p.tokens), p.flat_len};
+    seq_t s = {b, 1, 0};
+    if (p.q_starts) {
+        s.first = min(max(index_at(p.q_starts, b), 0), int(p.tokens));
+        s.n = min(min(max(index_at(p.q_starts, b + 1), s.first), int(p.tokens)) - s.first, p.max_q);
+    }
+    s.len = min(max(index_at(p.kv_lens, b), 0), p.max_kv);
+    return s;
+}
+
+// Byte offset in the pools of `token` of a sequence and of its 15 followers
+// (token % 16 == 0; pages hold whole multiples of 16).  `last` is the last page
+// of the sequence; a page number outside the pool is brought inside.
+__device__ __forceinline__ int64_t token_bytes(const attn_params &p, const int32_t *table, int token, int last, int head,
+                                               int dim) {
+    const uint32_t page = min(uint32_t(index_at(table, min(token >> p.page_shift, last))), p.pages - 1u);
+    const int64_t slot = ((int64_t(page) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
+    return slot * (2 * dim);
+}
+
+// LDS byte address of a pointer into a __shared__ array.
+__device__ __forceinline__ uint32_t lds_at(const uint8_t *p) {
+    return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint8_t *)p));
+}
+
+// Request 16 bytes a lane from base + off (base uniform) into LDS bytes dst + 16
+// lane (dst uniform).  In assembly, so that the compiler does not make every later
+// LDS read wait for every request: the kernels count them, and wait with
+// wait_loads before they read.  It has no register outputs.
+__device__ __forceinline__ void request_lds16(const void *base, uint32_t off, uint32_t dst) {
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                     :
+                     : "v"(off), "s"(base), "s"(dst)
+                     : "memory", "m0");
+}
+
+template <int DT>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (DT == 0)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <int DT>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (DT == 0)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Two FP32 values to a word of two elements, to nearest even.
+template <int DT>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+    if constexpr (DT == 0) {
+        typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, v2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
+    } else {
+        typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, v2{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+    }
+}
+
+// Four elements of one column from four rows of 16 (the transposing read): lane
+// i of each 16 names the 8 bytes at row i / 4, elements 4 (i % 4), and gets
+// element i of the four rows.
+__device__ __forceinline__ uint2 lds_tr(const uint8_t *p) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4 *)const_cast<uint8_t *>(p)));
+}
+
+__device__ __forceinline__ float max_over_32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_over_16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_over_32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum_over_16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Every LDS access of this wave has been answered; nothing moves across.
+__device__ __forceinline__ void wait_lds() {
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0); vmcnt and expcnt: no wait
+    __asm__ volatile("" ::: "memory");
+}
+
+// Raw products as scores in powers of two: capped, and biased by the distance of
+// their tokens.  tanh as 1 - 2 / (e^2x + 1): its absolute error, a few 2^-24,
+// times the cap is what a score's own rounding is.
+template <int N, typename Token>
+__device__ __forceinline__ void to_scores(const attn_params &p, float (&x)[N], float slope, int pos, Token token) {
+    if (p.softcap > 0.f) {
+        const float c = 2.f * kLog2e * p.scale / p.softcap, top = p.softcap * kLog2e;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            x[e] = top - 2.f * top * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * c) + 1.f);
+    } else {
+        const float c = p.scale * kLog2e;
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] *= c;
+    }
+    if (p.slopes) {
+        slope *= kLog2e;
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(slope, float(token(e) - pos), x[e]);
+    }
+}
+
+// Whether a word holds an infinity or a NaN in either half.
+template <int DT>
+__device__ __forceinline__ bool odd_word(uint32_t w) {
+    constexpr uint32_t e = DT == 0 ? 0x7f80u : 0x7c00u;
+    return (w & e) == e || (w & (e << 16)) == (e << 16);
+}
+
+// Tokens that a query does not see have weight 0, but 0 times an infinity or a
+// NaN is a NaN.  Where a tile has such values and queries that do not see all of
+// it, they are replaced by 0 in LDS, after the weights of +inf, -inf and NaN were
+// summed by products with indicators of each: a query that gives any of them
+// weight gets the value itself.
+enum { kFinite = 0, kPlus = 1, kMinus = 2, kNan = 3 };
+template <int DT, int KIND>
+__device__ __forceinline__ uint32_t only(uint32_t w) {
+    constexpr uint32_t e = DT == 0 ? 0x7f80u : 0x7c00u, one = DT == 0 ? 0x3f80u : 0x3c00u;
+    uint32_t r = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t x = (w >> (16 * h)) & 0xffffu, mag = x & 0x7fffu;
+        uint32_t y;
+        if constexpr (KIND == kFinite) y = mag >= e ? 0u : x;
+        else if constexpr (KIND == kPlus) y = x == e ? one : 0u;
+        else if constexpr (KIND == kMinus) y = x == (e | 0x8000u) ? one : 0u;
+        else y = mag > e ? one : 0u;
+        r |= y << (16 * h);
+    }
+    return r;
+}
+template <int DT, int KIND>
+__device__ __forceinline__ u32x4 only(u32x4 w) {
+    return u32x4{only<DT, KIND>(w[0]), only<DT, KIND>(w[1]), only<DT, KIND>(w[2]), only<DT, KIND>(w[3])};
+}
+template <int DT>
+__device__ __forceinline__ bool odd_words(u32x4 w) {
+    return odd_word<DT>(w[0]) || odd_word<DT>(w[1]) || odd_word<DT>(w[2]) || odd_word<DT>(w[3]);
+}
+template <int DT>
+__device__ __forceinline__ void add_odd(f32x4 &o, u32x4 val, u32x4 weights) {
+    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+    const f32x4 plus = mfma16<DT>(only<DT, kPlus>(val), weights, none);
+    const f32x4 minus = mfma16<DT>(only<DT, kMinus>(val), weights, none);
+    const f32x4 nan = mfma16<DT>(only<DT, kNan>(val), weights, none);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (plus[e] != 0.f) o[e] += __builtin_inff();
+        if (minus[e] != 0.f) o[e] -= __builtin_inff();
+        if (nan[e] != 0.f) o[e] = __builtin_nanf("");
+    }
+}
+
+// ---------------------------------------------------------------- launchers
+
+// Rows kernel: a tile of 16 nt rows (queries times the heads of a key head), the
+// tokens shared out over the waves and workgroups.
+struct rows_plan {
+    int nt;           // 16-row blocks of a tile
+    int grid;         // workgroups
+    int row_tiles;    // most row tiles of a sequence
+    int min_units;
+    bool split;       // a tile's tokens may be shared out over workgroups
+    int64_t numbers;  // sequences * key heads * row tiles
+    int64_t slots;    // of the workspace
+};
+hipError_t attn_rows_bf16_64(const rows_plan &r, const attn_params &p, hipStream_t stream);
+hipError_t attn_rows_bf16_128(const rows_plan &r, const attn_params &p, hipStream_t stream);
+hipError_t attn_rows_bf16_256(const rows_plan &r, const attn_params &p, hipStream_t stream);
+hipError_t attn_rows_fp16_64(const rows_plan &r, const attn_params &p, hipStream_t stream);
+hipError_t attn_rows_fp16_128(const rows_plan &r, const attn_params &p, hipStream_t stream);
+hipError_t attn_rows_fp16_256(const rows_plan &r, const attn_params &p, hipStream_t stream);
+
+// Where the parts of an output row are: part 0 at `first` + the number of its
+// (sequence, key head, row tile) or at `grid` + the workgroup that began it, the
+// next at the numbers of the workgroups that follow; or (splits > 0) all at
+// number * splits on.
+struct join_source {
+    const float *o, *ml;
+    const int2 *shares;
+    int rows;         // of a tile; 0: no such source
+    int row_tiles;
+    int grid, splits;
+    int64_t first;    // -1: parts begin at grid + workgroup
+};
+hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
+                            hipStream_t stream);
+
+}  // namespace cq

@@ -1,0 +1,124 @@
+// Joins the parts of an attention output that several workgroups hold: with the
+// largest of their maxima M, o = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k.
+// One wave for each query and head, the parts in order, so that the result does
+// not depend on which workgroup was done first.
+#include "a8_quant.h"
+#include "attn_common.h"
+
+namespace cq {
+
+namespace {
+
+// Slot of part k of `number`.
+__device__ __forceinline__ int64_t part_slot(const join_source &j, int64_t number, int first, int k) {
+    if (j.splits) return number * j.splits + k;
+    if (k == 0) return j.first >= 0 ? j.first + number : j.grid + int64_t(first);
+    return first + int64_t(k);
+}
+
+template <int DT, int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_source own, join_source flat) {
+    constexpr int E = D / kWave;
+    typedef float fE __attribute__((ext_vector_type(E)));
+    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= p.tokens * p.heads) return;
+    const int64_t token = row / p.heads;
+    const int head = int(row - token * p.heads), kvh = head / p.group, g = head - kvh * p.group;
+
+    // this row's place in each source
+    int64_t number[2] = {0, 0};
+    int at[2] = {0, 0}, first[2] = {0, 0}, count[2] = {0, 0};
+    if (own.rows) {
+        int b = int(token), begin = int(token);
+        if (p.q_starts) {
+            int lo = 0, hi = p.batch - 1;  // last b with q_starts[b] <= token
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (p.q_starts[mid] <= token) lo = mid; else hi = mid - 1;
+            }
+            b = lo;
+            const seq_t s = sequence(p, b);
+            begin = s.first;
+            if (token < begin || token >= begin + s.n) return;  // a row of no sequence
+        }
+        const int r = (int(token) - begin) * p.group + g, rt = r / own.rows;
+        number[0] = (int64_t(b) * p.kv_heads + kvh) * own.row_tiles + rt;
+        at[0] = r - rt * own.rows;
+        count[0] = own.splits;
+        if (!own.splits) {
+            const int2 s = own.shares[number[0]];
+            first[0] = s.x;
+            count[0] = s.y;
+        }
+    }
+    if (flat.rows) {
+        const int64_t r = token * p.group + g, rt = r / flat.rows;
+        number[1] = int64_t(kvh) * flat.row_tiles + rt;
+        at[1] = int(r - rt * flat.rows);
+        count[1] = flat.splits;
+        if (!flat.splits) {
+            const int2 s = flat.shares[number[1]];
+            first[1] = s.x;
+            count[1] = s.y;
+        }
+    }
+    const int parts = count[0] + count[1];
+    if (parts == 0) return;  // written whole
+    auto stat = [&](int k) {
+        const bool f = k >= count[0];
+        const join_source &j = f ? flat : own;
+        const int64_t slot = part_slot(j, number[f], first[f], f ? k - count[0] : k);
+        return *reinterpret_cast<const float2 *>(j.ml + (slot * j.rows + at[f]) * 2);
+    };
+    float top = kLowest;
+    for (int k = lane; k < parts; k += kWave) top = fmaxf(top, stat(k).x);
+    top = wave_max(top);
+    float sum = 0.f;
+    fE o = {};
+    for (int k0 = 0; k0 < parts; k0 += kWave) {
+        float scale = 0.f;
+        if (k0 + lane < parts) {
+            const float2 s = stat(k0 + lane);
+            scale = __builtin_amdgcn_exp2f(s.x - top);
+            sum += s.y * scale;
+        }
+        const int n = min(kWave, parts - k0);
+#pragma unroll 8
+        for (int k = 0; k < n; ++k) {
+            const bool f = k0 + k >= count[0];
+            const join_source &j = f ? flat : own;
+            const int64_t slot = part_slot(j, number[f], first[f], k0 + k - (f ? count[0] : 0));
+            const fE v = *reinterpret_cast<const fE *>(j.o + (slot * j.rows + at[f]) * D + lane * E);
+            o += v * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale), k));
+        }
+    }
+    sum = wave_sum(sum);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t *dst = p.out + row * D + lane * E;
+    if constexpr (E == 1) store_out<DT>(dst, 0, o[0] * inv);
+    else
+#pragma unroll
+        for (int e = 0; e < E; e += 2)
+            *reinterpret_cast<uint32_t *>(dst + e) = pack_pair<DT>(o[e] * inv, o[e + 1] * inv);
+}
+
+}  // namespace
+
+hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
+                            hipStream_t stream) {
+    const dim3 grid(uint32_t((p.tokens * p.heads + 3) / 4)), block(256);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, own, flat); };
+    if (dt == 0) {
+        if (dim == 64) go(attn_join_kernel<0, 64>);
+        else if (dim == 128) go(attn_join_kernel<0, 128>);
+        else go(attn_join_kernel<0, 256>);
+    } else {
+        if (dim == 64) go(attn_join_kernel<1, 64>);
+        else if (dim == 128) go(attn_join_kernel<1, 128>);
+        else go(attn_join_kernel<1, 256>);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cq

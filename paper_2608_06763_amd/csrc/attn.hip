@@ -23,44 +23,89 @@ rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
     return r;
 }
 
-struct source_bytes {
-    int64_t o, ml, shares;
-    int64_t all() const { return o + ml + shares; }
+// The wide kernel: at most `tiles` row tiles in all, few of which leave compute
+// units idle unless their tokens are split.
+wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens, bool keep) {
+    wide_plan w;
+    w.row_tiles = int((rows + 127) / 128);
+    w.tiles = all_rows / 128 + sequences;
+    const int64_t most = sequences * w.row_tiles;
+    if (w.tiles > most) w.tiles = most;
+    const int64_t slots = 2 * int64_t(device_cu_count());
+    int64_t splits = slots / (w.tiles * kv_heads), units = tokens / 256;  // four tiles of 64 at least
+    if (splits > units) splits = units;
+    w.splits = int(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+    w.slots = w.splits > 1 || keep ? sequences * kv_heads * w.row_tiles * w.splits : 0;
+    return w;
+}
+
+// One launch: of the rows kernel, or of the wide one.
+struct pass_plan {
+    bool wide, keep;
+    rows_plan rows;
+    wide_plan tall;
+    int64_t o, ml, shares;  // bytes of the workspace
+    int64_t bytes() const { return o + ml + shares; }
 };
-source_bytes bytes_of(const rows_plan &r, int dim, bool keep) {
+
+pass_plan plan_pass(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens,
+                    bool keep) {
+    pass_plan t;
+    t.keep = keep;
+    t.wide = rows > 64;
+    int64_t part_rows = 0;
+    t.shares = 0;
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
-    if (!r.split && !keep) return {0, 0, 0};
-    const int64_t rows = r.slots * 16 * r.nt;
-    return {up(rows * dim * 4), up(rows * 8), up(r.numbers * int64_t(sizeof(int2)))};
-}
-
-// Points a launch's parts at `ws`, and the join at them.
-join_source place(attn_params &p, const rows_plan &r, const source_bytes &n, bool keep, uint8_t *ws) {
-    p.part_o = reinterpret_cast<float *>(ws);
-    p.part_ml = reinterpret_cast<float *>(ws + n.o);
-    p.shares = n.shares ? reinterpret_cast<int2 *>(ws + n.o + n.ml) : nullptr;
-    p.row_tiles = r.row_tiles;
-    p.min_units = r.min_units;
-    p.keep_parts = keep;
-    join_source j = {p.part_o, p.part_ml, p.shares, n.shares ? 16 * r.nt : 0, r.row_tiles, r.grid, 0, -1};
-    if (keep) j.first = r.split ? 2 * int64_t(r.grid) : 0;
-    return j;
-}
-
-hipError_t launch_rows(int dt, int dim, const rows_plan &r, const attn_params &p, hipStream_t stream) {
-    if (dt == 0) {
-        if (dim == 64) return attn_rows_bf16_64(r, p, stream);
-        return dim == 128 ? attn_rows_bf16_128(r, p, stream) : attn_rows_bf16_256(r, p, stream);
+    if (t.wide) {
+        t.tall = plan_wide(sequences, kv_heads, rows, all_rows, tokens, keep);
+        part_rows = t.tall.slots * 128;
+    } else {
+        t.rows = plan_rows(dim, sequences, kv_heads, rows, tokens, keep);
+        if (t.rows.split || keep) {
+            part_rows = t.rows.slots * 16 * t.rows.nt;
+            t.shares = up(t.rows.numbers * int64_t(sizeof(int2)));
+        }
     }
-    if (dim == 64) return attn_rows_fp16_64(r, p, stream);
-    return dim == 128 ? attn_rows_fp16_128(r, p, stream) : attn_rows_fp16_256(r, p, stream);
+    t.o = up(part_rows * dim * 4);
+    t.ml = up(part_rows * 8);
+    return t;
+}
+
+hipError_t launch_pass(int dt, int dim, const pass_plan &t, attn_params p, uint8_t *ws, join_source *join,
+                       hipStream_t stream) {
+    typedef hipError_t (*rows_fn)(const rows_plan &, const attn_params &, hipStream_t);
+    typedef hipError_t (*wide_fn)(const wide_plan &, const attn_params &, hipStream_t);
+    static constexpr rows_fn rows_of[2][3] = {{attn_rows_bf16_64, attn_rows_bf16_128, attn_rows_bf16_256},
+                                              {attn_rows_fp16_64, attn_rows_fp16_128, attn_rows_fp16_256}};
+    static constexpr wide_fn wide_of[2][3] = {{attn_wide_bf16_64, attn_wide_bf16_128, attn_wide_bf16_256},
+                                              {attn_wide_fp16_64, attn_wide_fp16_128, attn_wide_fp16_256}};
+    const int d = dim == 64 ? 0 : dim == 128 ? 1 : 2;
+    p.part_o = reinterpret_cast<float *>(ws);
+    p.part_ml = reinterpret_cast<float *>(ws + t.o);
+    p.keep_parts = t.keep;
+    *join = {};
+    join->o = p.part_o;
+    join->ml = p.part_ml;
+    if (t.wide) {
+        p.row_tiles = join->row_tiles = t.tall.row_tiles;
+        join->splits = t.tall.splits;
+        join->rows = t.tall.slots ? 128 : 0;
+        return wide_of[dt][d](t.tall, p, stream);
+    }
+    p.row_tiles = join->row_tiles = t.rows.row_tiles;
+    p.min_units = t.rows.min_units;
+    p.shares = t.shares ? reinterpret_cast<int2 *>(ws + t.o + t.ml) : nullptr;
+    join->shares = p.shares;
+    join->rows = t.shares ? 16 * t.rows.nt : 0;
+    join->grid = t.rows.grid;
+    join->first = !t.keep ? -1 : t.rows.split ? 2 * int64_t(t.rows.grid) : 0;
+    return rows_of[dt][d](t.rows, p, stream);
 }
 
 struct plan_t {
-    rows_plan own, flat;
-    source_bytes own_bytes, flat_bytes;
+    pass_plan own, flat;
     bool shared;
-    int64_t max_kv;
+    int64_t max_kv, flat_bytes;
 };
 
 plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
@@ -68,12 +113,12 @@ plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
     const int64_t group = a.heads / c.kv_heads, held = int64_t(a.table_width) * c.page;
     t.max_kv = a.max_kv < held ? a.max_kv : held;
     t.shared = a.prefix_len > 0;
-    t.own = plan_rows(c.dim, a.batch, c.kv_heads, a.max_q * group, t.max_kv, t.shared);
-    t.own_bytes = bytes_of(t.own, c.dim, t.shared);
-    t.flat_bytes = {0, 0, 0};
+    const int64_t rows = a.tokens * group;
+    t.own = plan_pass(c.dim, a.batch, c.kv_heads, a.max_q * group, rows, t.max_kv, t.shared);
+    t.flat_bytes = 0;
     if (t.shared) {
-        t.flat = plan_rows(c.dim, 1, c.kv_heads, a.tokens * group, a.prefix_len, true);
-        t.flat_bytes = bytes_of(t.flat, c.dim, true);
+        t.flat = plan_pass(c.dim, 1, c.kv_heads, rows, rows, a.prefix_len, true);
+        t.flat_bytes = t.flat.bytes();
     }
     return t;
 }
@@ -82,7 +127,7 @@ plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
 
 int64_t attn_workspace_bytes(const cq_kv_cache &c, const cq_attn_args &a) {
     const plan_t t = make_plan(c, a);
-    return t.own_bytes.all() + t.flat_bytes.all();
+    return t.own.bytes() + t.flat_bytes;
 }
 
 hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *workspace, hipStream_t stream) {
@@ -113,21 +158,18 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     p.softcap = a.softcap;
 
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    join_source flat = {};
+    join_source own, flat = {};
     if (t.shared) {
         attn_params f = p;
         f.flat = 1;
         f.flat_len = int(a.prefix_len);
         f.tables = a.prefix_table;
-        f.kv_lens = f.bidir = nullptr;
-        f.q_starts = nullptr;
+        f.kv_lens = f.q_starts = nullptr;
         f.batch = 1;
-        flat = place(f, t.flat, t.flat_bytes, true, ws + t.own_bytes.all());
-        const hipError_t e = launch_rows(int(c.dtype), c.dim, t.flat, f, stream);
+        const hipError_t e = launch_pass(int(c.dtype), c.dim, t.flat, f, ws + t.own.bytes(), &flat, stream);
         if (e != hipSuccess) return e;
     }
-    const join_source own = place(p, t.own, t.own_bytes, t.shared, ws);
-    const hipError_t e = launch_rows(int(c.dtype), c.dim, t.own, p, stream);
+    const hipError_t e = launch_pass(int(c.dtype), c.dim, t.own, p, ws, &own, stream);
     if (e != hipSuccess || !own.rows) return e;
     return launch_attn_join(int(c.dtype), c.dim, p, own, flat, stream);
 }

@@ -259,18 +259,32 @@ template <int DT>
 __device__ __forceinline__ bool odd_words(u32x4 w) {
     return odd_word<DT>(w[0]) || odd_word<DT>(w[1]) || odd_word<DT>(w[2]) || odd_word<DT>(w[3]);
 }
-template <int DT>
-__device__ __forceinline__ void add_odd(f32x4 &o, u32x4 val, u32x4 weights) {
-    const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-    const f32x4 plus = mfma16<DT>(only<DT, kPlus>(val), weights, none);
-    const f32x4 minus = mfma16<DT>(only<DT, kMinus>(val), weights, none);
-    const f32x4 nan = mfma16<DT>(only<DT, kNan>(val), weights, none);
+template <int DT, typename Acc>
+__device__ __forceinline__ void add_odd(Acc &o, u32x4 val, u32x4 weights) {
+    constexpr int N = sizeof(Acc) / 4;
+    auto product = [&](u32x4 v) {
+        Acc none = {};
+        if constexpr (N == 4) return mfma16<DT>(v, weights, none);
+        else return mfma32<DT>(v, weights, none);
+    };
+    auto add = [&](u32x4 v, float value) {
+        const Acc seen = product(v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (plus[e] != 0.f) o[e] += __builtin_inff();
-        if (minus[e] != 0.f) o[e] -= __builtin_inff();
-        if (nan[e] != 0.f) o[e] = __builtin_nanf("");
-    }
+        for (int e = 0; e < N; ++e) o[e] += seen[e] != 0.f ? value : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    add(only<DT, kPlus>(val), __builtin_inff());
+    add(only<DT, kMinus>(val), -__builtin_inff());
+    add(only<DT, kNan>(val), __builtin_nanf(""));
+}
+
+// Tiles keep the tokens' rows in LDS, their 16-byte chunks in an order of their own:
+// chunk c of a row lies at place c ^ key_place(row) (K) or c ^ val_place(row) (V,
+// for each kernel), which takes the rows that one LDS read visits to different
+// banks.  The requests permute the chunks inside a row, so LDS is written in order.
+template <int D>
+__device__ __forceinline__ constexpr int key_place(int row) {  // 16 rows, 16 bytes of each
+    return D == 64 ? (row >> 1) & 7 : row & 15;
 }
 
 // ---------------------------------------------------------------- launchers
@@ -292,6 +306,20 @@ hipError_t attn_rows_bf16_256(const rows_plan &r, const attn_params &p, hipStrea
 hipError_t attn_rows_fp16_64(const rows_plan &r, const attn_params &p, hipStream_t stream);
 hipError_t attn_rows_fp16_128(const rows_plan &r, const attn_params &p, hipStream_t stream);
 hipError_t attn_rows_fp16_256(const rows_plan &r, const attn_params &p, hipStream_t stream);
+
+// Wide kernel: tiles of 128 rows; `splits` workgroups share the tokens of each.
+struct wide_plan {
+    int64_t tiles;    // most row tiles of all sequences
+    int row_tiles;    // most of one
+    int splits;
+    int64_t slots;
+};
+hipError_t attn_wide_bf16_64(const wide_plan &w, const attn_params &p, hipStream_t stream);
+hipError_t attn_wide_bf16_128(const wide_plan &w, const attn_params &p, hipStream_t stream);
+hipError_t attn_wide_bf16_256(const wide_plan &w, const attn_params &p, hipStream_t stream);
+hipError_t attn_wide_fp16_64(const wide_plan &w, const attn_params &p, hipStream_t stream);
+hipError_t attn_wide_fp16_128(const wide_plan &w, const attn_params &p, hipStream_t stream);
+hipError_t attn_wide_fp16_256(const wide_plan &w, const attn_params &p, hipStream_t stream);
 
 // Where the parts of an output row are: part 0 at `first` + the number of its
 // (sequence, key head, row tile) or at `grid` + the workgroup that began it, the

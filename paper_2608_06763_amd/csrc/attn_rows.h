@@ -15,11 +15,7 @@
 namespace cq {
 
 template <int D>
-__device__ __forceinline__ constexpr int row_key(int row) {  // 16-byte chunks of K: 16 rows, 16 places
-    return D == 64 ? (row >> 1) & 7 : row & 15;
-}
-template <int D>
-__device__ __forceinline__ constexpr int row_val(int row) {  // of V: 8 rows, 32 bytes each
+__device__ __forceinline__ constexpr int val_place(int row) {  // of V: 8 rows, 32 bytes each
     return D == 64 ? 2 * ((row >> 1) & 3) : 2 * (row & 7);
 }
 
@@ -52,10 +48,13 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
         b = fixed / (p.kv_heads * p.row_tiles);
     } else {
         const int me = blockIdx.x;
-        const place_t at = locate(p, R, -1, [&](int64_t all) {
-            const int n = sharers(p, all, grid);
-            return me < n ? first_unit(all, n, me) : int64_t(-1);
-        }, sched);
+        const place_t at = locate(
+            p.flat ? 1 : p.batch, [&](int b) { return work_of(p, sequence(p, b), R).total; },
+            [&](int64_t all) {
+                const int n = sharers(p, all, grid);
+                return me < n ? first_unit(all, n, me) : int64_t(-1);
+            },
+            sched);
         total = at.total;
         sharing = sharers(p, total, grid);
         if (me >= sharing || total == 0) return;
@@ -141,8 +140,8 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
                 }
             }
         };
-        auto request_k = [&](int t) { request(p.k, lds_at(ks), t, [](int row) { return row_key<D>(row); }); };
-        auto request_v = [&](int t) { request(p.v, lds_at(vs), t, [](int row) { return row_val<D>(row); }); };
+        auto request_k = [&](int t) { request(p.k, lds_at(ks), t, [](int row) { return key_place<D>(row); }); };
+        auto request_v = [&](int t) { request(p.v, lds_at(vs), t, [](int row) { return val_place<D>(row); }); };
 
         int t = w.tile0 + t_begin + wave;
         if (t < t1) {
@@ -177,7 +176,7 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const int row = 16 * g + col;
-                    const u32x4 key = *reinterpret_cast<const u32x4 *>(ks + row * (2 * D) + (((4 * k + quad) ^ row_key<D>(row)) << 4));
+                    const u32x4 key = *reinterpret_cast<const u32x4 *>(ks + row * (2 * D) + (((4 * k + quad) ^ key_place<D>(row)) << 4));
 #pragma unroll
                     for (int n = 0; n < NT; ++n) sc[n][g] = mfma16<DT>(key, q[n][k], sc[n][g]);
                 }
@@ -240,7 +239,7 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const int row = 16 * g + 4 * quad + (col >> 2), byte = 32 * d + 8 * (col & 3);
-                    const uint2 v = lds_tr(vs + row * (2 * D) + (((byte >> 4) ^ row_val<D>(row)) << 4) + (byte & 15));
+                    const uint2 v = lds_tr(vs + row * (2 * D) + (((byte >> 4) ^ val_place<D>(row)) << 4) + (byte & 15));
                     val[2 * g] = v.x;
                     val[2 * g + 1] = v.y;
                 }

@@ -29,24 +29,24 @@ __device__ __forceinline__ work_t work_of(const attn_params &p, const seq_t &s, 
     return w;
 }
 
-// Units in all, and where unit u (or where sequence b begins) lies.
+// Units in all, and the sequence that holds one of them.
 struct place_t {
-    int64_t total;   // units of the launch
-    int b;           // the sequence of the first unit of this workgroup
+    int64_t total;
+    int b;
     int64_t before;  // units before sequence b
 };
 
-// All 256 threads call it; `lds` is 64 bytes.  find >= 0: the sequence that holds
-// unit find(total); else `b` is given and `before` is found.
-template <typename Find>
-__device__ __forceinline__ place_t locate(const attn_params &p, int rows, int given, Find find, uint8_t *lds) {
+// All 256 threads call it; `lds` is 64 bytes.  Sequence b has count(b) units; the
+// one that holds unit find(total) is found.
+template <typename Count, typename Find>
+__device__ __forceinline__ place_t locate(int n, Count count, Find find, uint8_t *lds) {
     int64_t *sums = reinterpret_cast<int64_t *>(lds);         // 4 wave sums
     int64_t *found = reinterpret_cast<int64_t *>(lds) + 4;    // units before it
     int *found_b = reinterpret_cast<int *>(lds + 40);
-    const int n = p.flat ? 1 : p.batch, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (n + 255) / 256, lo = min(tid * per, n), hi = min(lo + per, n);
     int64_t own = 0;
-    for (int b = lo; b < hi; ++b) own += work_of(p, sequence(p, b), rows).total;
+    for (int b = lo; b < hi; ++b) own += count(b);
     int64_t run = own;  // inclusive sum over the wave
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -63,23 +63,18 @@ __device__ __forceinline__ place_t locate(const attn_params &p, int rows, int gi
     }
     int64_t at = base + run - own;
     const int64_t u = find(total);
-    const bool mine = given >= 0 ? (given >= lo && given < hi) : (u >= at && u < at + own);
-    if (mine) {
+    if (u >= at && u < at + own) {
         int b = lo;
         for (; b < hi - 1; ++b) {
-            const int64_t t = work_of(p, sequence(p, b), rows).total;
-            if (given >= 0 ? b == given : u < at + t) break;
+            const int64_t t = count(b);
+            if (u < at + t) break;
             at += t;
         }
         *found = at;
         *found_b = b;
     }
     __syncthreads();
-    place_t r;
-    r.total = total;
-    r.before = *found;
-    r.b = *found_b;
-    return r;
+    return {total, *found_b, *found};
 }
 
 // Workgroups that share `total` units, and the first unit of workgroup w.

@@ -231,51 +231,38 @@ __device__ __forceinline__ bool odd_word(uint32_t w) {
 
 // Tokens that a query does not see have weight 0, but 0 times an infinity or a
 // NaN is a NaN.  Where a tile has such values and queries that do not see all of
-// it, they are replaced by 0 in LDS, after the weights of +inf, -inf and NaN were
-// summed by products with indicators of each: a query that gives any of them
-// weight gets the value itself.
-enum { kFinite = 0, kPlus = 1, kMinus = 2, kNan = 3 };
-template <int DT, int KIND>
-__device__ __forceinline__ uint32_t only(uint32_t w) {
-    constexpr uint32_t e = DT == 0 ? 0x7f80u : 0x7c00u, one = DT == 0 ? 0x3f80u : 0x3c00u;
-    uint32_t r = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t x = (w >> (16 * h)) & 0xffffu, mag = x & 0x7fffu;
-        uint32_t y;
-        if constexpr (KIND == kFinite) y = mag >= e ? 0u : x;
-        else if constexpr (KIND == kPlus) y = x == e ? one : 0u;
-        else if constexpr (KIND == kMinus) y = x == (e | 0x8000u) ? one : 0u;
-        else y = mag > e ? one : 0u;
-        r |= y << (16 * h);
-    }
-    return r;
-}
-template <int DT, int KIND>
-__device__ __forceinline__ u32x4 only(u32x4 w) {
-    return u32x4{only<DT, KIND>(w[0]), only<DT, KIND>(w[1]), only<DT, KIND>(w[2]), only<DT, KIND>(w[3])};
-}
+// it, the products take V with them replaced by 0, and the weights of +inf, -inf
+// and NaN are summed by products with indicators of each: a query that gives any
+// of them weight gets the value itself.
 template <int DT>
 __device__ __forceinline__ bool odd_words(u32x4 w) {
     return odd_word<DT>(w[0]) || odd_word<DT>(w[1]) || odd_word<DT>(w[2]) || odd_word<DT>(w[3]);
 }
-template <int DT, typename Acc>
-__device__ __forceinline__ void add_odd(Acc &o, u32x4 val, u32x4 weights) {
-    constexpr int N = sizeof(Acc) / 4;
-    auto product = [&](u32x4 v) {
-        Acc none = {};
-        if constexpr (N == 4) return mfma16<DT>(v, weights, none);
-        else return mfma32<DT>(v, weights, none);
-    };
-    auto add = [&](u32x4 v, float value) {
-        const Acc seen = product(v);
+template <int DT>
+__device__ __forceinline__ u32x4 finite_only(u32x4 w) {
+    constexpr uint32_t e = DT == 0 ? 0x7f80u : 0x7c00u;
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] += seen[e] != 0.f ? value : 0.f;
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    add(only<DT, kPlus>(val), __builtin_inff());
-    add(only<DT, kMinus>(val), -__builtin_inff());
-    add(only<DT, kNan>(val), __builtin_nanf(""));
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & e) == e) w[i] &= 0xffff0000u;
+        if ((w[i] & (e << 16)) == (e << 16)) w[i] &= 0xffffu;
+    }
+    return w;
+}
+// 1 where a value is +inf, -inf or NaN (kind 0, 1, 2), else 0
+template <int DT>
+__device__ __forceinline__ u32x4 odd_ones(u32x4 w, int kind) {
+    constexpr uint32_t e = DT == 0 ? 0x7f80u : 0x7c00u, one = DT == 0 ? 0x3f80u : 0x3c00u;
+    const uint32_t keep = kind == 2 ? 0x7fffu : 0xffffu;
+    const uint32_t lo = kind == 0 ? e : kind == 1 ? e | 0x8000u : e + 1, hi = kind == 2 ? 0x7fffu : lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = w[i] & keep, b = (w[i] >> 16) & keep;
+        w[i] = (a >= lo && a <= hi ? one : 0u) | (b >= lo && b <= hi ? one << 16 : 0u);
+    }
+    return w;
+}
+__device__ __forceinline__ float odd_value(int kind) {
+    return kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
 }
 
 // Tiles keep the tokens' rows in LDS, their 16-byte chunks in an order of their own:

@@ -1,7 +1,7 @@
 // Joins the parts of an attention output that several workgroups hold: with the
 // largest of their maxima M, o = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k.
-// One wave for each query and head, the parts in order, so that the result does
-// not depend on which workgroup was done first.
+// One workgroup for each query and head, the parts in an order of their own, so
+// that the result does not depend on which workgroup was done first.
 #include "a8_quant.h"
 #include "attn_common.h"
 
@@ -16,13 +16,15 @@ __device__ __forceinline__ int64_t part_slot(const join_source &j, int64_t numbe
     return first + int64_t(k);
 }
 
+constexpr int kBatch = 8;
+
 template <int DT, int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_source own, join_source flat) {
     constexpr int E = D / kWave;
     typedef float fE __attribute__((ext_vector_type(E)));
-    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= p.tokens * p.heads) return;
+    __shared__ float share[3][D + 4];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t token = row / p.heads;
     const int head = int(row - token * p.heads), kvh = head / p.group, g = head - kvh * p.group;
 
@@ -65,35 +67,55 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
     }
     const int parts = count[0] + count[1];
     if (parts == 0) return;  // written whole
-    auto stat = [&](int k) {
+    auto slot_of = [&](int k) {
         const bool f = k >= count[0];
         const join_source &j = f ? flat : own;
-        const int64_t slot = part_slot(j, number[f], first[f], f ? k - count[0] : k);
-        return *reinterpret_cast<const float2 *>(j.ml + (slot * j.rows + at[f]) * 2);
+        return (part_slot(j, number[f], first[f], f ? k - count[0] : k) * j.rows + at[f]);
     };
+    auto stat = [&](int k) {
+        return *reinterpret_cast<const float2 *>((k >= count[0] ? flat.ml : own.ml) + slot_of(k) * 2);
+    };
+    // every wave has all maxima; the parts themselves are shared out, kBatch
+    // requests of a wave at a time
     float top = kLowest;
     for (int k = lane; k < parts; k += kWave) top = fmaxf(top, stat(k).x);
     top = wave_max(top);
     float sum = 0.f;
     fE o = {};
-    for (int k0 = 0; k0 < parts; k0 += kWave) {
+    for (int k0 = wave * kBatch; k0 < parts; k0 += 4 * kBatch) {
         float scale = 0.f;
-        if (k0 + lane < parts) {
+        if (lane < kBatch && k0 + lane < parts) {
             const float2 s = stat(k0 + lane);
             scale = __builtin_amdgcn_exp2f(s.x - top);
             sum += s.y * scale;
         }
-        const int n = min(kWave, parts - k0);
-#pragma unroll 8
-        for (int k = 0; k < n; ++k) {
-            const bool f = k0 + k >= count[0];
-            const join_source &j = f ? flat : own;
-            const int64_t slot = part_slot(j, number[f], first[f], k0 + k - (f ? count[0] : 0));
-            const fE v = *reinterpret_cast<const fE *>(j.o + (slot * j.rows + at[f]) * D + lane * E);
-            o += v * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale), k));
+        fE v[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int kk = min(k0 + k, parts - 1);
+            v[k] = *reinterpret_cast<const fE *>((kk >= count[0] ? flat.o : own.o) + slot_of(kk) * D + lane * E);
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale), k));
+            if (k0 + k < parts) o += v[k] * w;
         }
     }
     sum = wave_sum(sum);
+    if (parts > kBatch) {  // the other waves have a share (uniform)
+        if (wave) {
+            *reinterpret_cast<fE *>(&share[wave - 1][lane * E]) = o;
+            if (lane == 0) share[wave - 1][D] = sum;
+        }
+        __syncthreads();
+        if (wave == 0)
+#pragma unroll
+            for (int w = 0; w < 3; ++w) {
+                o += *reinterpret_cast<const fE *>(&share[w][lane * E]);
+                sum += share[w][D];
+            }
+    }
+    if (wave) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     uint16_t *dst = p.out + row * D + lane * E;
     if constexpr (E == 1) store_out<DT>(dst, 0, o[0] * inv);
@@ -107,7 +129,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
                             hipStream_t stream) {
-    const dim3 grid(uint32_t((p.tokens * p.heads + 3) / 4)), block(256);
+    const dim3 grid(uint32_t(p.tokens * p.heads)), block(256);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, own, flat); };
     if (dt == 0) {
         if (dim == 64) go(attn_join_kernel<0, 64>);

@@ -35,33 +35,33 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
     __shared__ __align__(1024) uint8_t stage_k[4 * kTile];
     __shared__ __align__(1024) uint8_t stage_v[4 * kTile];
     __shared__ float stat[4][NT][2][64];
-    __shared__ __align__(16) uint8_t sched[64];
+    __shared__ int sched[8];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
     uint8_t *const ks = stage_k + wave * kTile, *const vs = stage_v + wave * kTile;
 
-    int64_t u = 0, u_end = 1, total = 1, before = 0;
-    int b = 0, sharing = 1, fixed = -1;
+    int u = 0, u_end = 1, before = 0, b = 0;
+    runs_t runs = {1, 1, 0};
+    const int fixed = blockIdx.x;
     if (direct) {
-        fixed = blockIdx.x;
         b = fixed / (p.kv_heads * p.row_tiles);
     } else {
         const int me = blockIdx.x;
         const place_t at = locate(
             p.flat ? 1 : p.batch, [&](int b) { return work_of(p, sequence(p, b), R).total; },
-            [&](int64_t all) {
-                const int n = sharers(p, all, grid);
-                return me < n ? first_unit(all, n, me) : int64_t(-1);
+            [&](int all) {
+                const runs_t r = runs_of(p, all, grid);
+                return me < r.n ? r.first(me) : -1;
             },
             sched);
-        total = at.total;
-        sharing = sharers(p, total, grid);
-        if (me >= sharing || total == 0) return;
-        u = first_unit(total, sharing, me);
-        u_end = first_unit(total, sharing, me + 1);
+        const int total = __builtin_amdgcn_readfirstlane(at.total);
+        runs = runs_of(p, total, grid);
+        if (me >= runs.n || total == 0) return;
+        u = runs.first(me);
+        u_end = runs.first(me + 1);
         b = __builtin_amdgcn_readfirstlane(at.b);
-        before = at.before;
+        before = __builtin_amdgcn_readfirstlane(at.before);
     }
 
     while (u < u_end) {
@@ -82,13 +82,13 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
                 ++b;
                 continue;
             }
-            const int64_t in = u - before;
-            part = int(in / w.units);
-            t_begin = int(in - int64_t(part) * w.units);
-            t_end = int(min(int64_t(w.units), t_begin + (u_end - u)));
+            const int in = u - before;
+            part = in / w.units;
+            t_begin = in - part * w.units;
+            t_end = min(w.units, t_begin + (u_end - u));
         }
-        const int head = direct ? part / p.row_tiles : part / w.row_tiles;
-        const int rt = direct ? part % p.row_tiles : part % w.row_tiles;
+        const int tiles_of = direct ? p.row_tiles : w.row_tiles;
+        const int head = part / tiles_of, rt = part - head * tiles_of;
         const int64_t number = part_number(p, b, head, rt);
 
         // ---- the rows of this tile
@@ -250,16 +250,36 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) odd |= odd_words<DT>(*reinterpret_cast<const u32x4 *>(vs + i * 1024 + lane * 16));
                 if (__any(odd)) {
+                    // bit 4 d + e of seen: element e of o[n][d] gets this value
+#pragma unroll 1
+                    for (int kind = 0; kind < 3; ++kind) {
+                        uint64_t seen[NT] = {};
+#pragma unroll 1
+                        for (int d = 0; d < OT; ++d) {
+                            const u32x4 val = odd_ones<DT>(values(d), kind);
 #pragma unroll
-                    for (int d = 0; d < OT; ++d) {
-                        const u32x4 val = values(d);
+                            for (int n = 0; n < NT; ++n) {
+                                const f32x4 mass = mfma16<DT>(val, u32x4{wt[n][0], wt[n][1], wt[n][2], wt[n][3]},
+                                                              f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) add_odd<DT>(o[n][d], val, u32x4{wt[n][0], wt[n][1], wt[n][2], wt[n][3]});
+                                for (int e = 0; e < 4; ++e) seen[n] |= uint64_t(mass[e] != 0.f) << (4 * d + e);
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            if (__any(seen[n] != 0)) {
+#pragma unroll
+                                for (int d = 0; d < OT; ++d)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        o[n][d][e] += (seen[n] >> (4 * d + e)) & 1 ? odd_value(kind) : 0.f;
+                            }
                     }
                     wait_lds();
+#pragma unroll 1
                     for (int i = 0; i < kLoads; ++i) {
                         u32x4 *at = reinterpret_cast<u32x4 *>(vs + i * 1024 + lane * 16);
-                        *at = only<DT, kFinite>(*at);
+                        *at = finite_only<DT>(*at);
                     }
                     wait_lds();
                 }
@@ -320,7 +340,7 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
             else if (!complete) slot = t_begin == 0 ? grid + int64_t(blockIdx.x) : int64_t(blockIdx.x);
             if (t_begin == 0 && lane == 0 && p.shares) {
                 // who holds the parts: the first workgroup and how many (0: written whole)
-                int count = complete ? 1 : holder(total, sharing, u + w.units - 1) - int(blockIdx.x) + 1;
+                int count = complete ? 1 : runs.holder(u + w.units - 1) - int(blockIdx.x) + 1;
                 if (complete && !p.keep_parts) count = 0;
                 p.shares[number] = make_int2(int(blockIdx.x), count);
             }

@@ -30,7 +30,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
     constexpr float kLift = DT == 0 ? 0.f : 10.f;  // as in the rows kernel
     __shared__ __align__(1024) uint8_t stage_k[2 * kTile];
     __shared__ __align__(1024) uint8_t stage_v[2 * kTile];
-    __shared__ __align__(16) uint8_t sched[64];
+    __shared__ int sched[8];
+    __shared__ int odd_tile[2][4];  // a wave found infinities or NaNs in its part of V
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -38,14 +39,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
     // ---- which rows: the tiles of a key head go to one XCD where there are eight
     // heads or more, and the ones with the most tokens come first
     const int head = blockIdx.x % p.kv_heads, split = blockIdx.y;
-    const int64_t tile = blockIdx.x / p.kv_heads;
-    auto tiles_of = [&](int b) { return int64_t((sequence(p, b).n * p.group + kWideRows - 1) / kWideRows); };
-    const place_t at = locate(p.flat ? 1 : p.batch, tiles_of, [&](int64_t) { return tile; }, sched);
+    const int tile = blockIdx.x / p.kv_heads;
+    auto tiles_of = [&](int b) { return (sequence(p, b).n * p.group + kWideRows - 1) / kWideRows; };
+    const place_t at = locate(p.flat ? 1 : p.batch, tiles_of, [&](int) { return tile; }, sched);
     if (tile >= at.total) return;
     const int b = __builtin_amdgcn_readfirstlane(at.b);
     const seq_t s = sequence_uniform(p, b);
     const int last_rt = (s.n * p.group + kWideRows - 1) / kWideRows - 1;
-    const int rt = last_rt - __builtin_amdgcn_readfirstlane(int(tile - at.before));
+    const int rt = last_rt - __builtin_amdgcn_readfirstlane(tile - at.before);
     const int bidir = p.bidir ? min(index_at(p.bidir, b), s.len) : 0;
     const int r0 = rt * kWideRows, rows = min(kWideRows, s.n * p.group - r0);
     const int pos0 = s.len - s.n;  // position of the first query
@@ -154,8 +155,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
             auto token = [&](int e) { return a + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3); };
             if constexpr (GEN) to_scores(p, x, slope, lim.pos, token);
             if (!whole) {
+                // against the tile's first token of this half: constants on the other side
+                const limits_t rel = {lim.hi - a - 4 * half, lim.lo - a - 4 * half, lim.bi - a - 4 * half, 0};
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = sees(lim, token(e)) ? x[e] : -__builtin_inff();
+                for (int e = 0; e < 32; ++e)
+                    x[e] = sees(rel, 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3)) ? x[e] : -__builtin_inff();
             }
 #pragma unroll
             for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
@@ -179,14 +183,21 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
         }
         // ---- values have arrived
         if (more) wait_loads<kLoads>(); else wait_loads<0>();
-        if (a + kWideTile > s.len) {  // rows of no token hold anything: zeros, each wave its own
+        // Does any row of the workgroup not see all of the tile?  Then each wave looks
+        // at the values that it brought: rows of no token hold anything and become
+        // zeros, other infinities and NaNs are marked.
+        const bool mixed = a + kWideTile > s.len || (!p.flat && (a + kWideTile > lo_pos + 1 || (p.window && a <= hi_pos - p.window)));
+        if (mixed) {
+            bool odd = false;
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
                 const int row = 16 * wave + n * kPerLoad + lane / kChunks;
-                if (a + row >= s.len)
-                    *reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16) =
-                        u32x4{0, 0, 0, 0};
+                u32x4 *v = reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
+                if (a + row >= s.len) *v = u32x4{0, 0, 0, 0};
+                else odd |= odd_words<DT>(*v);
             }
+            odd = __any(odd);
+            if (lane == 0) odd_tile[t & 1][wave] = odd;
             wait_lds();
         }
         __builtin_amdgcn_s_barrier();
@@ -212,25 +223,38 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
         };
         bool odd = false;
         if (!whole && !p.flat) {
-#pragma unroll 4
-            for (int n = 0; n < kTile / 1024; ++n)
-                odd |= odd_words<DT>(*reinterpret_cast<const u32x4 *>(vs + n * 1024 + lane * 16));
-            odd = __any(odd);
+            const int *f = odd_tile[t & 1];
+            odd = __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
         }
         if (!odd) {
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
                 for (int d = 0; d < OT; ++d) o[d] = mfma32<DT>(values(d, n), weights(n), o[d]);
-        } else {
+            continue;
+        }
+        // seldom run: little code and few registers
+#pragma unroll 1
+        for (int n = 0; n < 4; ++n) {
+            u32x4 w = weights(0);
 #pragma unroll
-            for (int d = 0; d < OT; ++d)
+            for (int k = 1; k < 4; ++k)
+                if (n == k) w = weights(k);
+#pragma unroll 1
+            for (int kind = -1; kind < 3; ++kind)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
+                for (int d = 0; d < OT; ++d) {
+                    vmem_order();
                     const u32x4 val = values(d, n);
-                    o[d] = mfma32<DT>(only<DT, kFinite>(val), weights(n), o[d]);
-                    add_odd<DT>(o[d], val, weights(n));
-                    __builtin_amdgcn_sched_barrier(0);  // seldom run: few registers, whatever the order
+                    if (kind < 0) {
+                        o[d] = mfma32<DT>(finite_only<DT>(val), w, o[d]);
+                    } else {
+                        f32x16 mass = {};
+                        mass = mfma32<DT>(odd_ones<DT>(val, kind), w, mass);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[d][e] += mass[e] != 0.f ? odd_value(kind) : 0.f;
+                    }
+                    vmem_order();
                 }
         }
     }

@@ -9,14 +9,14 @@ namespace {
 // The rows kernel for `sequences` of at most `rows` rows and `tokens` tokens.
 rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t tokens, bool keep) {
     rows_plan r;
-    r.nt = rows <= 16 ? 1 : rows <= 32 || dim == 256 ? 2 : 4;
+    r.nt = rows <= 16 ? 1 : 2;
     r.row_tiles = int((rows + 16 * r.nt - 1) / (16 * r.nt));
     r.numbers = sequences * kv_heads * r.row_tiles;
     const int64_t units = tokens > 32 ? (tokens + 31) / 32 : 1;
     r.min_units = 4;
-    r.split = units > 8;
+    r.split = units > 16;
     // workgroups that LDS and registers let run at once
-    const int64_t most = int64_t(device_cu_count()) * (dim == 256 || r.nt == 4 ? 1 : 2);
+    const int64_t most = int64_t(device_cu_count()) * (dim == 256 ? 1 : 2);
     const int64_t need = (r.numbers * units + r.min_units - 1) / r.min_units;
     r.grid = int(r.split ? (need < most ? need : most) : r.numbers);
     r.slots = (r.split ? 2 * int64_t(r.grid) : 0) + (keep ? r.numbers : 0);
@@ -52,7 +52,7 @@ pass_plan plan_pass(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
                     bool keep) {
     pass_plan t;
     t.keep = keep;
-    t.wide = rows > 64;
+    t.wide = rows > 32;
     int64_t part_rows = 0;
     t.shares = 0;
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };

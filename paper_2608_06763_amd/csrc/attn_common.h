@@ -114,13 +114,17 @@ __device__ __forceinline__ seq_t sequence_uniform(const attn_params &p, int b) {
     return s;
 }
 
-// Byte offset in the pools of `token` of a sequence and of its 15 followers
-// (token % 16 == 0; pages hold whole multiples of 16).  `last` is the last page
-// of the sequence; a page number outside the pool is brought inside.
-__device__ __forceinline__ int64_t token_bytes(const attn_params &p, const int32_t *table, int token, int last, int head,
-                                               int dim) {
-    const uint32_t page = min(uint32_t(index_at(table, min(token >> p.page_shift, last))), p.pages - 1u);
-    const int64_t slot = ((int64_t(page) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
+// The page of `token`; past the sequence's `last` page, that one.  The kernels ask
+// for it a tile ahead, so that its answer is there when the tile is requested.
+__device__ __forceinline__ int page_of(const attn_params &p, const int32_t *table, int token, int last) {
+    return index_at(table, min(token >> p.page_shift, last));
+}
+
+// Byte offset in the pools of `token` and its 15 followers (token % 16 == 0; pages
+// hold whole multiples of 16).  A page number outside the pool is brought inside.
+__device__ __forceinline__ int64_t token_bytes(const attn_params &p, int page, int token, int head, int dim) {
+    const uint32_t inside = min(uint32_t(page), p.pages - 1u);
+    const int64_t slot = ((int64_t(inside) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
     return slot * (2 * dim);
 }
 

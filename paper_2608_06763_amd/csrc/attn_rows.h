@@ -20,7 +20,7 @@ __device__ __forceinline__ constexpr int val_place(int row) {  // of V: 8 rows, 
 }
 
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_kernel(attn_params p, int grid, int direct) {
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_params p, int grid, int direct) {
     constexpr int kTile = kUnit * D * 2;          // bytes of 32 tokens
     constexpr int kLoads = kTile / 1024;          // a wave's requests for them
     constexpr int kChunks = D / 8;                // 16-byte chunks of a token
@@ -126,12 +126,10 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
         const int first_pos = s.len - s.n, last_pos = s.len - 1;
         // tokens below this are seen by no row
         const int lo_all = p.window && !p.bidir && !p.flat ? max(0, first_pos - p.window + 1) : 0;
-        auto request = [&](const uint16_t *pool, uint32_t dst, int t, auto place) {
-            const int token = t * kUnit;
+        auto request = [&](const uint16_t *pool, uint32_t dst, const int64_t (&at)[2], auto place) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const uint8_t *base = reinterpret_cast<const uint8_t *>(pool) +
-                                      token_bytes(p, table, token + 16 * half, last, head, D);
+                const uint8_t *base = reinterpret_cast<const uint8_t *>(pool) + at[half];
 #pragma unroll
                 for (int i = 0; i < kLoads / 2; ++i) {
                     const int row = i * kPerLoad + lane / kChunks;  // of 16; places repeat after 16 rows
@@ -140,15 +138,33 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
                 }
             }
         };
-        auto request_k = [&](int t) { request(p.k, lds_at(ks), t, [](int row) { return key_place<D>(row); }); };
-        auto request_v = [&](int t) { request(p.v, lds_at(vs), t, [](int row) { return val_place<D>(row); }); };
+        auto request_k = [&](const int64_t (&at)[2]) {
+            request(p.k, lds_at(ks), at, [](int row) { return key_place<D>(row); });
+        };
+        auto request_v = [&](const int64_t (&at)[2]) {
+            request(p.v, lds_at(vs), at, [](int row) { return val_place<D>(row); });
+        };
+        // pages of the two halves of tile t, and where they lie
+        int page[2];
+        int64_t at[2];
+        auto ask = [&](int t) {
+            page[0] = page_of(p, table, t * kUnit, last);
+            page[1] = page_of(p, table, t * kUnit + 16, last);
+        };
+        auto find = [&](int t) {
+            at[0] = token_bytes(p, page[0], t * kUnit, head, D);
+            at[1] = token_bytes(p, page[1], t * kUnit + 16, head, D);
+        };
 
         int t = w.tile0 + t_begin + wave;
         if (t < t1) {
-            request_k(t);
+            ask(t);
+            find(t);
+            request_k(at);
             vmem_order();
-            request_v(t);
+            request_v(at);
             vmem_order();
+            ask(t + 4);
         }
         // The queries after the first tile's requests, and waited for with them:
         // the loop then has no wait for a load but the counted ones.
@@ -182,8 +198,10 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
                 }
             // the keys are in registers: their place takes the next tile's
             wait_lds();
-            if (more) request_k(t + 4);
+            find(t + 4);
+            if (more) request_k(at);
             vmem_order();
+            ask(t + 8);
             // ---- softmax
             bool whole = p.flat ? a + kUnit <= s.len : a + kUnit <= first_pos + 1;
             if (!p.flat && p.window) whole = whole && a > last_pos - p.window;
@@ -295,7 +313,7 @@ __global__ void __launch_bounds__(256, NT == 4 || D == 256 ? 1 : 2) attn_rows_ke
                 }
             }
             wait_lds();
-            if (more) request_v(t + 4);
+            if (more) request_v(at);
             vmem_order();
         }
 
@@ -378,9 +396,7 @@ hipError_t attn_rows_dim(const rows_plan &r, const attn_params &p, hipStream_t s
     const dim3 grid(uint32_t(r.grid)), block(256);
     const int direct = r.split ? 0 : 1;
     if (r.nt == 1) hipLaunchKernelGGL((attn_rows_kernel<DT, D, 1>), grid, block, 0, stream, p, r.grid, direct);
-    else if (r.nt == 2) hipLaunchKernelGGL((attn_rows_kernel<DT, D, 2>), grid, block, 0, stream, p, r.grid, direct);
-    else if constexpr (D < 256) hipLaunchKernelGGL((attn_rows_kernel<DT, D, 4>), grid, block, 0, stream, p, r.grid, direct);
-    else return hipErrorInvalidValue;
+    else hipLaunchKernelGGL((attn_rows_kernel<DT, D, 2>), grid, block, 0, stream, p, r.grid, direct);
     return hipGetLastError();
 }
 

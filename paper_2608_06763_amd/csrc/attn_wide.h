@@ -3,7 +3,7 @@
 //
 // Bound by the matrix cores and by the softmax between the two products.  A
 // workgroup takes 128 rows (queries times the heads of a key head), 32 a wave, and
-// walks the tokens in tiles of 64 that its waves share through LDS: keys and values
+// walks the tokens in tiles of 64 (32 of 256 channels) that its waves share through LDS: keys and values
 // have two places each, so that a tile's requests are out while the one before is
 // used.  Two workgroups on a compute unit run the products of the one beside the
 // softmax of the other.
@@ -13,7 +13,7 @@
 
 namespace cq {
 
-constexpr int kWideRows = 128, kWideTile = 64;
+constexpr int kWideRows = 128;
 
 template <int D>
 __device__ __forceinline__ constexpr int wide_val(int row) {  // 16-byte chunks of V: 4 rows, 64 bytes each
@@ -23,7 +23,9 @@ __device__ __forceinline__ constexpr int wide_val(int row) {  // 16-byte chunks 
 // GEN: scores are capped or biased.
 template <int DT, int D, bool GEN>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_params p, int splits) {
-    constexpr int kTile = kWideTile * D * 2;
+    constexpr int TK = D == 256 ? 32 : 64;  // tokens of a tile
+    constexpr int SB = TK / 32;
+    constexpr int kTile = TK * D * 2;
     constexpr int kLoads = kTile / 4096;    // requests of one wave for a tile
     constexpr int kChunks = D / 8, kPerLoad = 64 / kChunks;
     constexpr int KS = D / 16, OT = D / 32;
@@ -62,7 +64,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
         end = min(s.len, max(hi_pos + 1, hi_pos >= 0 ? bidir : 0));
         if (p.window && bidir <= 0) begin = max(0, lo_pos - p.window + 1);
     }
-    int t = begin / kWideTile, t1 = end > begin ? (end + kWideTile - 1) / kWideTile : begin / kWideTile;
+    int t = begin / TK, t1 = end > begin ? (end + TK - 1) / TK : begin / TK;
     if (splits > 1) {
         const int n = t1 - t, first = t;
         t = first + int(int64_t(n) * split / splits);
@@ -71,28 +73,34 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
 
     const int32_t *table = p.flat ? p.tables : p.tables + int64_t(b) * p.table_width;
     const int last = (s.len - 1) >> p.page_shift;
-    // Wave w requests tokens 16 w .. of a tile; inside 16 tokens the pages are one run.
-    auto request = [&](const uint16_t *pool, uint32_t dst, int tt, auto place) {
-        const uint8_t *base = reinterpret_cast<const uint8_t *>(pool) +
-                              token_bytes(p, table, tt * kWideTile + 16 * wave, last, head, D);
+    // Wave w requests tokens TK / 4 w .. of a tile; inside 16 tokens the pages are one run.
+    auto request = [&](const uint16_t *pool, uint32_t dst, int64_t at, auto place) {
+        const uint8_t *base = reinterpret_cast<const uint8_t *>(pool) + at;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = i * kPerLoad + lane / kChunks;
+            const int row = TK / 4 * wave + i * kPerLoad + lane / kChunks;
             const int chunk = (lane % kChunks) ^ place(row);
-            request_lds16(base, uint32_t(row * (2 * D) + chunk * 16), dst + wave * (kTile / 4) + i * 1024);
+            request_lds16(base, uint32_t((row - TK / 4 * wave) * (2 * D) + chunk * 16), dst + wave * (kTile / 4) + i * 1024);
         }
     };
-    auto request_k = [&](int tt) {
-        request(p.k, lds_at(stage_k) + (tt & 1) * kTile, tt, [](int row) { return key_place<D>(row); });
+    auto request_k = [&](int tt, int64_t at) {
+        request(p.k, lds_at(stage_k) + (tt & 1) * kTile, at, [](int row) { return key_place<D>(row); });
     };
-    auto request_v = [&](int tt) {
-        request(p.v, lds_at(stage_v) + (tt & 1) * kTile, tt, [](int row) { return wide_val<D>(row); });
+    auto request_v = [&](int tt, int64_t at) {
+        request(p.v, lds_at(stage_v) + (tt & 1) * kTile, at, [](int row) { return wide_val<D>(row); });
     };
+    int page = 0;
+    int64_t next = 0;
+    auto ask = [&](int tt) { page = page_of(p, table, tt * TK + TK / 4 * wave, last); };
+    auto find = [&](int tt) { next = token_bytes(p, page, tt * TK + TK / 4 * wave, head, D); };
     if (t < t1) {
-        request_k(t);
+        ask(t);
+        find(t);
+        request_k(t, next);
         vmem_order();
-        request_v(t);
+        request_v(t, next);
         vmem_order();
+        ask(t + 1);
     }
 
     // ---- this lane's query
@@ -121,24 +129,26 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
     const float c = GEN ? 1.f : p.scale * kLog2e;
 
     for (; t < t1; ++t) {
-        const int a = t * kWideTile;
+        const int a = t * TK;
         const bool more = t + 1 < t1;
         const uint8_t *ks = stage_k + (t & 1) * kTile, *vs = stage_v + (t & 1) * kTile;
         // ---- keys have arrived; every wave is done with the other place
         wait_loads<kLoads>();
         __builtin_amdgcn_s_barrier();
-        if (more) request_k(t + 1);
+        find(t + 1);
+        if (more) request_k(t + 1, next);
         vmem_order();
+        ask(t + 2);
         // does the wave see any of the tile, and all of it?
         const bool skip = idle || (!p.flat && a > wave_hi && a >= bidir) ||
-                          (!p.flat && p.window && a + kWideTile <= wave_lo - p.window + 1 && a >= bidir);
-        bool whole = p.flat ? a + kWideTile <= s.len : a + kWideTile <= wave_lo + 1;
+                          (!p.flat && p.window && a + TK <= wave_lo - p.window + 1 && a >= bidir);
+        bool whole = p.flat ? a + TK <= s.len : a + TK <= wave_lo + 1;
         if (!p.flat && p.window) whole = whole && a > wave_hi - p.window;
-        uint32_t wt[2][8];
+        uint32_t wt[SB][8];
         if (!skip) {
-            f32x16 sc[2];
+            f32x16 sc[SB];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
+            for (int g = 0; g < SB; ++g) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[g][e] = 0.f;
                 const int row = 32 * g + col;
@@ -149,20 +159,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
                 }
             }
             // ---- softmax
-            float x[32], top = kLowest;
+            float x[16 * SB], top = kLowest;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = sc[e >> 4][e & 15];
+            for (int e = 0; e < 16 * SB; ++e) x[e] = sc[e >> 4][e & 15];
             auto token = [&](int e) { return a + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3); };
             if constexpr (GEN) to_scores(p, x, slope, lim.pos, token);
             if (!whole) {
                 // against the tile's first token of this half: constants on the other side
                 const limits_t rel = {lim.hi - a - 4 * half, lim.lo - a - 4 * half, lim.bi - a - 4 * half, 0};
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
+                for (int e = 0; e < 16 * SB; ++e)
                     x[e] = sees(rel, 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3)) ? x[e] : -__builtin_inff();
             }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+            for (int e = 0; e < 16 * SB; ++e) top = fmaxf(top, x[e]);
             top = max_over_32(top) * c;
             if (__any(top > m + kSlack)) {
                 const float now = fmaxf(m, top), scale = __builtin_amdgcn_exp2f(m - now);
@@ -173,25 +183,25 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
             }
             const float shift = m - kLift;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -shift));
+            for (int e = 0; e < 16 * SB; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -shift));
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 32; ++e) sum[e & 3] += x[e];
+            for (int e = 0; e < 16 * SB; ++e) sum[e & 3] += x[e];
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) wt[e >> 3][e & 7] = pack_pair<DT>(x[2 * e], x[2 * e + 1]);
+            for (int e = 0; e < 8 * SB; ++e) wt[e >> 3][e & 7] = pack_pair<DT>(x[2 * e], x[2 * e + 1]);
         }
         // ---- values have arrived
         if (more) wait_loads<kLoads>(); else wait_loads<0>();
         // Does any row of the workgroup not see all of the tile?  Then each wave looks
         // at the values that it brought: rows of no token hold anything and become
         // zeros, other infinities and NaNs are marked.
-        const bool mixed = a + kWideTile > s.len || (!p.flat && (a + kWideTile > lo_pos + 1 || (p.window && a <= hi_pos - p.window)));
+        const bool mixed = a + TK > s.len || (!p.flat && (a + TK > lo_pos + 1 || (p.window && a <= hi_pos - p.window)));
         if (mixed) {
             bool odd = false;
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
-                const int row = 16 * wave + n * kPerLoad + lane / kChunks;
+                const int row = TK / 4 * wave + n * kPerLoad + lane / kChunks;
                 u32x4 *v = reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
                 if (a + row >= s.len) *v = u32x4{0, 0, 0, 0};
                 else odd |= odd_words<DT>(*v);
@@ -201,9 +211,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
             wait_lds();
         }
         __builtin_amdgcn_s_barrier();
-        if (more) request_v(t + 1);
+        if (more) request_v(t + 1, next);
         vmem_order();
-        if (skip) continue;
         // four tokens of one channel twice: the rows that k-step n of the lane's half holds
         auto values = [&](int d, int n) {
             u32x4 val;
@@ -221,42 +230,52 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_wide_kernel(attn_p
             const uint32_t *w = &wt[n >> 1][4 * (n & 1)];
             return u32x4{w[0], w[1], w[2], w[3]};
         };
-        bool odd = false;
-        if (!whole && !p.flat) {
+        if (mixed && !p.flat) {
             const int *f = odd_tile[t & 1];
-            odd = __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
-        }
-        if (!odd) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int d = 0; d < OT; ++d) o[d] = mfma32<DT>(values(d, n), weights(n), o[d]);
-            continue;
-        }
-        // seldom run: little code and few registers
+            if (__builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3])) {  // uniform over the workgroup; seldom
+                if (!skip) {
 #pragma unroll 1
-        for (int n = 0; n < 4; ++n) {
-            u32x4 w = weights(0);
+                    for (int kind = 0; kind < 3; ++kind) {
+                        uint32_t seen[OT];  // bit e of seen[d]: element e of o[d] gets this value
 #pragma unroll
-            for (int k = 1; k < 4; ++k)
-                if (n == k) w = weights(k);
-#pragma unroll 1
-            for (int kind = -1; kind < 3; ++kind)
+                        for (int d = 0; d < OT; ++d) {
+                            f32x16 mass = {};
 #pragma unroll
-                for (int d = 0; d < OT; ++d) {
-                    vmem_order();
-                    const u32x4 val = values(d, n);
-                    if (kind < 0) {
-                        o[d] = mfma32<DT>(finite_only<DT>(val), w, o[d]);
-                    } else {
-                        f32x16 mass = {};
-                        mass = mfma32<DT>(odd_ones<DT>(val, kind), w, mass);
+                            for (int n = 0; n < 2 * SB; ++n) {
+                                vmem_order();
+                                mass = mfma32<DT>(odd_ones<DT>(values(d, n), kind), weights(n), mass);
+                            }
+                            seen[d] = 0;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[d][e] += mass[e] != 0.f ? odd_value(kind) : 0.f;
+                            for (int e = 0; e < 16; ++e) seen[d] |= uint32_t(mass[e] != 0.f) << e;
+                            vmem_order();
+                        }
+#pragma unroll
+                        for (int d = 0; d < OT; ++d)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                o[d][e] += (seen[d] >> e) & 1 ? odd_value(kind) : 0.f;
+                                if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                            }
                     }
-                    vmem_order();
                 }
+                __builtin_amdgcn_s_barrier();
+                vmem_order();
+#pragma unroll 1
+                for (int n = 0; n < kLoads; ++n) {
+                    u32x4 *v = reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
+                    *v = finite_only<DT>(*v);
+                }
+                wait_lds();
+                __builtin_amdgcn_s_barrier();
+                vmem_order();
+            }
         }
+        if (skip) continue;
+#pragma unroll
+        for (int n = 0; n < 2 * SB; ++n)
+#pragma unroll
+            for (int d = 0; d < OT; ++d) o[d] = mfma32<DT>(values(d, n), weights(n), o[d]);
     }
 
     // ---- the wave's rows

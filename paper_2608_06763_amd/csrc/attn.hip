@@ -31,9 +31,9 @@ wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_r
     w.tiles = all_rows / 128 + sequences;
     const int64_t most = sequences * w.row_tiles;
     if (w.tiles > most) w.tiles = most;
-    const int64_t slots = 2 * int64_t(device_cu_count());
-    int64_t splits = slots / (w.tiles * kv_heads), units = tokens / 256;  // four tiles of 64 at least
-    if (splits > units) splits = units;
+    const int64_t units = tokens / 256, groups = w.tiles * kv_heads, cus = device_cu_count();
+    int64_t splits = groups >= cus ? 1 : 2 * cus / groups;
+    if (splits > units) splits = units;  // four tiles of 64 at least
     w.splits = int(splits < 1 ? 1 : splits > 64 ? 64 : splits);
     w.slots = w.splits > 1 || keep ? sequences * kv_heads * w.row_tiles * w.splits : 0;
     return w;
@@ -171,7 +171,7 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     }
     const hipError_t e = launch_pass(int(c.dtype), c.dim, t.own, p, ws, &own, stream);
     if (e != hipSuccess || !own.rows) return e;
-    return launch_attn_join(int(c.dtype), c.dim, p, own, flat, stream);
+    return launch_attn_join(int(c.dtype), c.dim, p, own, flat, p.tokens * p.heads >= 4096, stream);
 }
 
 }  // namespace cq

@@ -114,10 +114,15 @@ __device__ __forceinline__ seq_t sequence_uniform(const attn_params &p, int b) {
     return s;
 }
 
-// The page of `token`; past the sequence's `last` page, that one.  The kernels ask
-// for it a tile ahead, so that its answer is there when the tile is requested.
-__device__ __forceinline__ int page_of(const attn_params &p, const int32_t *table, int token, int last) {
-    return index_at(table, min(token >> p.page_shift, last));
+// Pages of 64 tiles ahead, one in each lane: a tile's page is then a register read.
+// (A scalar load would come back out of order with the LDS reads, and every wait for
+// one of those would wait for it.)  Tile i of the 64 begins at token `from` + i *
+// `step`; past the sequence's `last` page, that one.
+__device__ __forceinline__ int pages_ahead(const attn_params &p, const int32_t *table, int from, int step, int last) {
+    const int64_t token = from + int64_t(step) * (threadIdx.x & 63);
+    int page = table[min(token >> p.page_shift, int64_t(last))];
+    __asm__ volatile("" : "+v"(page));  // waited for here, and not at every use
+    return page;
 }
 
 // Byte offset in the pools of `token` and its 15 followers (token % 16 == 0; pages
@@ -169,6 +174,18 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
     } else {
         typedef _Float16 v2 __attribute__((ext_vector_type(2)));
         return __builtin_bit_cast(uint32_t, v2{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+    }
+}
+
+// c plus both elements of a word, exact but for the sum's rounding.
+template <int DT>
+__device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    if constexpr (DT == 0) {
+        typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, w), v2{1.0f, 1.0f}, c, false);
+    } else {
+        typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2, w), v2{1.0f, 1.0f}, c, false);
     }
 }
 
@@ -325,6 +342,6 @@ struct join_source {
     int64_t first;    // -1: parts begin at grid + workgroup
 };
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
-                            hipStream_t stream);
+                            bool few, hipStream_t stream);
 
 }  // namespace cq

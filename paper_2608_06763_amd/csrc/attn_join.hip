@@ -16,15 +16,17 @@ __device__ __forceinline__ int64_t part_slot(const join_source &j, int64_t numbe
     return first + int64_t(k);
 }
 
-constexpr int kBatch = 8;
-
-template <int DT, int D>
+// W waves share a row's parts; 4 / W rows to a workgroup.
+template <int DT, int D, int W>
 __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_source own, join_source flat) {
     constexpr int E = D / kWave;
     typedef float fE __attribute__((ext_vector_type(E)));
+    constexpr int kBatch = W == 1 ? 2 : 8;  // requests of a wave at a time
     __shared__ float share[3][D + 4];
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % W;
+    const int64_t row = int64_t(blockIdx.x) * (4 / W) + id / W;
+    const int lane = threadIdx.x & 63;
+    if (row >= p.tokens * p.heads) return;
     const int64_t token = row / p.heads;
     const int head = int(row - token * p.heads), kvh = head / p.group, g = head - kvh * p.group;
 
@@ -82,7 +84,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
     top = wave_max(top);
     float sum = 0.f;
     fE o = {};
-    for (int k0 = wave * kBatch; k0 < parts; k0 += 4 * kBatch) {
+    for (int k0 = wave * kBatch; k0 < parts; k0 += W * kBatch) {
         float scale = 0.f;
         if (lane < kBatch && k0 + lane < parts) {
             const float2 s = stat(k0 + lane);
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
         }
     }
     sum = wave_sum(sum);
-    if (parts > kBatch) {  // the other waves have a share (uniform)
+    if (W > 1 && parts > kBatch) {  // the other waves have a share (uniform)
         if (wave) {
             *reinterpret_cast<fE *>(&share[wave - 1][lane * E]) = o;
             if (lane == 0) share[wave - 1][D] = sum;
@@ -127,18 +129,20 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 
 }  // namespace
 
+// One wave a row where a row has few parts or the rows fill the chip; else four.
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
-                            hipStream_t stream) {
-    const dim3 grid(uint32_t(p.tokens * p.heads)), block(256);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, own, flat); };
+                            bool few, hipStream_t stream) {
+    const int64_t rows = p.tokens * p.heads;
+    const dim3 grid(uint32_t(few ? (rows + 3) / 4 : rows)), block(256);
+    auto go = [&](auto one, auto four) { hipLaunchKernelGGL(few ? one : four, grid, block, 0, stream, p, own, flat); };
     if (dt == 0) {
-        if (dim == 64) go(attn_join_kernel<0, 64>);
-        else if (dim == 128) go(attn_join_kernel<0, 128>);
-        else go(attn_join_kernel<0, 256>);
+        if (dim == 64) go(attn_join_kernel<0, 64, 1>, attn_join_kernel<0, 64, 4>);
+        else if (dim == 128) go(attn_join_kernel<0, 128, 1>, attn_join_kernel<0, 128, 4>);
+        else go(attn_join_kernel<0, 256, 1>, attn_join_kernel<0, 256, 4>);
     } else {
-        if (dim == 64) go(attn_join_kernel<1, 64>);
-        else if (dim == 128) go(attn_join_kernel<1, 128>);
-        else go(attn_join_kernel<1, 256>);
+        if (dim == 64) go(attn_join_kernel<1, 64, 1>, attn_join_kernel<1, 64, 4>);
+        else if (dim == 128) go(attn_join_kernel<1, 128, 1>, attn_join_kernel<1, 128, 4>);
+        else go(attn_join_kernel<1, 256, 1>, attn_join_kernel<1, 256, 4>);
     }
     return hipGetLastError();
 }

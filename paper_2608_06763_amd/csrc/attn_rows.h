@@ -144,27 +144,29 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
         auto request_v = [&](const int64_t (&at)[2]) {
             request(p.v, lds_at(vs), at, [](int row) { return val_place<D>(row); });
         };
-        // pages of the two halves of tile t, and where they lie
-        int page[2];
+        // where the two halves of tile t lie; this wave's tiles are four apart
+        int pages[2] = {0, 0}, pages_from = 0;
         int64_t at[2];
-        auto ask = [&](int t) {
-            page[0] = page_of(p, table, t * kUnit, last);
-            page[1] = page_of(p, table, t * kUnit + 16, last);
+        auto look = [&](int t) {
+            pages_from = t;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) pages[h] = pages_ahead(p, table, t * kUnit + 16 * h, 4 * kUnit, last);
         };
         auto find = [&](int t) {
-            at[0] = token_bytes(p, page[0], t * kUnit, head, D);
-            at[1] = token_bytes(p, page[1], t * kUnit + 16, head, D);
+            if (t - pages_from >= 4 * 64) look(t);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                at[h] = token_bytes(p, __builtin_amdgcn_readlane(pages[h], (t - pages_from) >> 2), t * kUnit + 16 * h, head, D);
         };
 
         int t = w.tile0 + t_begin + wave;
         if (t < t1) {
-            ask(t);
+            look(t);
             find(t);
             request_k(at);
             vmem_order();
             request_v(at);
             vmem_order();
-            ask(t + 4);
         }
         // The queries after the first tile's requests, and waited for with them:
         // the loop then has no wait for a load but the counted ones.
@@ -198,10 +200,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
                 }
             // the keys are in registers: their place takes the next tile's
             wait_lds();
-            find(t + 4);
-            if (more) request_k(at);
+            if (more) {
+                find(t + 4);
+                request_k(at);
+            }
             vmem_order();
-            ask(t + 8);
             // ---- softmax
             bool whole = p.flat ? a + kUnit <= s.len : a + kUnit <= first_pos + 1;
             if (!p.flat && p.window) whole = whole && a > last_pos - p.window;

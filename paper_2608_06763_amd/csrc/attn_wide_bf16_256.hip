@@ -1,10 +1,10 @@
-// attn_wide.h for BF16 heads of 256.
-#include "attn_wide.h"
+// attn_wide_256.h for BF16 heads of 256.
+#include "attn_wide_256.h"
 
 namespace cq {
 
 hipError_t attn_wide_bf16_256(const wide_plan &w, const attn_params &p, hipStream_t stream) {
-    return attn_wide_dim<0, 256>(w, p, stream);
+    return attn_wide_256_dim<0>(w, p, stream);
 }
 
 }  // namespace cq

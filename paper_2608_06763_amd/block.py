@@ -6,8 +6,9 @@ two tensors [pages, kv_heads, page, dim] that the caller owns.
 from __future__ import annotations
 
 import ctypes
+import struct
 
-from . import CQ_BF16, CQ_FP16, CQ_FP32, _check, _dt, _stream_ptr, _torch, lib
+from . import CQ_BF16, CQ_FP16, CQ_FP32, CQError, _stream_ptr, _torch, lib
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -37,56 +38,98 @@ class cq_attn_args(ctypes.Structure):
                 ("bidir", _vp), ("prefix_table", _vp), ("prefix_len", _i64)]
 
 
+# The same structures as bytes: the calls pack their arguments in one step, which
+# takes a third of the time of filling a ctypes structure field by field.
+_NORM = struct.Struct("@7P3q2i3f")
+_CACHE = struct.Struct("@4iq2P")
+_ROPE = struct.Struct("@4P4q4P2q3i")
+_ATTN = struct.Struct("@2P2q2i2P3iP2fi3Pq")
+for _s, _c in ((_NORM, cq_norm_args), (_CACHE, cq_kv_cache), (_ROPE, cq_rope_args), (_ATTN, cq_attn_args)):
+    # C pads a structure at its end too
+    assert (_s.size + 7) // 8 * 8 == ctypes.sizeof(_c), _c
+
+
 def declare(L):
-    """Argument types of the entry points in a loaded library."""
-    P = ctypes.POINTER
-    for name, args in (("cq_norm_residual", [P(cq_norm_args), _vp]),
-                       ("cq_norm_residual_a8", [P(cq_norm_args), _vp, _vp, _vp]),
-                       ("cq_rope_append", [P(cq_kv_cache), P(cq_rope_args), _vp]),
-                       ("cq_attn_paged", [P(cq_kv_cache), P(cq_attn_args), _vp, _i64, _vp]),
-                       ("cq_attn_shared_prefix", [P(cq_kv_cache), P(cq_attn_args), _vp, _i64, _vp])):
+    """Argument types of the entry points in a loaded library (structures by address)."""
+    for name, args in (("cq_norm_residual", [_vp, _vp]),
+                       ("cq_norm_residual_a8", [_vp, _vp, _vp, _vp]),
+                       ("cq_rope_append", [_vp, _vp, _vp]),
+                       ("cq_attn_paged", [_vp, _vp, _vp, _i64, _vp]),
+                       ("cq_attn_shared_prefix", [_vp, _vp, _vp, _i64, _vp])):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = args
     L.cq_attn_workspace_bytes.restype = _i64
-    L.cq_attn_workspace_bytes.argtypes = [P(cq_kv_cache), P(cq_attn_args)]
+    L.cq_attn_workspace_bytes.argtypes = [_vp, _vp]
+
+
+_types = None
+
+
+def _type(t):
+    """dtype code of a tensor."""
+    global _types
+    if _types is None:
+        torch = _torch()
+        _types = {torch.bfloat16: CQ_BF16, torch.float16: CQ_FP16, torch.float32: CQ_FP32}
+    code = _types.get(t.dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return code
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
+
+
+def _dense(t, like):
+    """t has the shape and type of `like` and is contiguous."""
+    assert t.dtype == like.dtype and t.shape == like.shape and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _vector(t, size, dtype):
+    assert t.dtype == dtype and t.shape == (size,) and t.is_contiguous()
+    return t.data_ptr()
 
 
 # ---------------------------------------------------------------- norms
 
 
 def _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out):
-    torch = _torch()
     rows, width = residual.shape
-    assert residual.is_contiguous() and weight.shape == (width,) and weight.is_contiguous()
-    dtype, stride = weight.dtype, 0
+    dtype = weight.dtype
+    assert residual.is_contiguous()
+    y_at = post = gate_at = stride = out_at = r_at = 0
+    r = residual
     if y is not None:
-        assert y.shape == residual.shape and y.is_contiguous() and y.dtype == dtype
+        assert y.dtype == dtype and y.shape == residual.shape and y.is_contiguous()
+        y_at = y.data_ptr()
         if residual_out is None:
-            residual_out = torch.empty_like(residual)
-        assert residual_out.shape == residual.shape and residual_out.is_contiguous()
-        assert residual_out.dtype == residual.dtype
+            r = _torch().empty_like(residual)
+            r_at = r.data_ptr()
+        else:
+            r = residual_out
+            r_at = _dense(r, residual)
         if post_weight is not None:
-            assert post_weight.shape == (width,) and post_weight.is_contiguous() and post_weight.dtype == dtype
+            post = _vector(post_weight, width, dtype)
         if gate is not None:
             # one gate for all rows, or a row for each
-            assert gate.shape[-1] == width and gate.stride(-1) == 1 and gate.dtype == dtype
+            assert gate.dtype == dtype and gate.shape[-1] == width and gate.stride(-1) == 1
             if gate.dim() == 2:
                 assert gate.shape[0] == rows
-                stride = gate.stride(0)
+                # the stride of a single row is never used: any legal one serves
+                stride = gate.stride(0) if rows > 1 else width
             else:
                 assert gate.dim() == 1
+            gate_at = gate.data_ptr()
     else:
         assert post_weight is None and gate is None and residual_out is None
     if out is not None:
-        assert out.shape == residual.shape and out.is_contiguous() and out.dtype == dtype
-    args = cq_norm_args(_ptr(y), _ptr(post_weight), _ptr(gate), residual.data_ptr(), weight.data_ptr(),
-                        _ptr(residual_out), _ptr(out), stride, rows, width, _dt(dtype), _dt(residual.dtype), alpha,
-                        eps, weight_offset)
-    return args, residual if y is None else residual_out
+        assert out.dtype == dtype and out.shape == residual.shape and out.is_contiguous()
+        out_at = out.data_ptr()
+    args = _NORM.pack(y_at, post, gate_at, residual.data_ptr(), _vector(weight, width, dtype), r_at, out_at, stride,
+                      rows, width, _type(weight), _type(residual), alpha, eps, weight_offset)
+    return args, r
 
 
 def cq_norm_residual(residual, weight, eps, y=None, post_weight=None, gate=None, alpha=1.0, weight_offset=0.0,
@@ -98,9 +141,11 @@ def cq_norm_residual(residual, weight, eps, y=None, post_weight=None, gate=None,
     dtype.  Without y, r' is the residual itself.  residual_out may be residual,
     out may be y."""
     if out is None:
-        out = _torch().empty(residual.shape, dtype=weight.dtype, device=residual.device)
+        out = _torch().empty_like(residual, dtype=weight.dtype)
     args, r = _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out)
-    _check(lib().cq_norm_residual(ctypes.byref(args), _stream_ptr(stream)), "cq_norm_residual")
+    st = lib().cq_norm_residual(args, _stream_ptr(stream))
+    if st:
+        raise CQError(st, "cq_norm_residual")
     return out, r
 
 
@@ -109,15 +154,16 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
     """cq_norm_residual with h straight to the Dynamic-A8 carriers; returns
     (x8, dx, r').  h itself is written only into a given out."""
     torch = _torch()
+    rows = residual.shape[0]
     if x8 is None:
-        x8 = torch.empty(residual.shape, dtype=torch.int8, device=residual.device)
+        x8 = torch.empty_like(residual, dtype=torch.int8)
     if dx is None:
-        dx = torch.empty((residual.shape[0],), dtype=torch.float32, device=residual.device)
+        dx = torch.empty((rows,), dtype=torch.float32, device=residual.device)
     assert x8.shape == residual.shape and x8.is_contiguous() and x8.dtype == torch.int8
-    assert dx.shape == (residual.shape[0],) and dx.is_contiguous() and dx.dtype == torch.float32
     args, r = _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out)
-    st = lib().cq_norm_residual_a8(ctypes.byref(args), x8.data_ptr(), dx.data_ptr(), _stream_ptr(stream))
-    _check(st, "cq_norm_residual_a8")
+    st = lib().cq_norm_residual_a8(args, x8.data_ptr(), _vector(dx, rows, torch.float32), _stream_ptr(stream))
+    if st:
+        raise CQError(st, "cq_norm_residual_a8")
     return x8, dx, r
 
 
@@ -126,23 +172,17 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
 
 def _cache(k_cache, v_cache):
     pages, kv_heads, page, dim = k_cache.shape
-    assert v_cache.shape == k_cache.shape and k_cache.is_contiguous() and v_cache.is_contiguous()
-    assert v_cache.dtype == k_cache.dtype
-    return cq_kv_cache(_dt(k_cache.dtype), kv_heads, dim, page, pages, k_cache.data_ptr(), v_cache.data_ptr())
+    assert k_cache.is_contiguous()
+    return _CACHE.pack(_type(k_cache), kv_heads, dim, page, pages, k_cache.data_ptr(), _dense(v_cache, k_cache)), kv_heads, dim
 
 
-def _heads_stride(x, dtype, dim):
+def _heads_stride(x, dtype, heads, dim):
     """Stride between tokens of x [tokens, heads, dim], whose heads are dense."""
     token, head, one = x.stride()
-    assert x.dtype == dtype and x.shape[2] == dim and one == 1 and (head == dim or x.shape[1] == 1)
+    tokens, n, d = x.shape
+    assert x.dtype == dtype and n == heads and d == dim and one == 1 and (head == dim or n == 1)
     # the stride of a single token is never used: any legal one serves
-    return token if x.shape[0] > 1 else max(token, x.shape[1] * dim)
-
-
-def _index(t, shape):
-    torch = _torch()
-    assert t.dtype == torch.int32 and t.is_contiguous() and t.shape == shape
-    return t.data_ptr()
+    return token if tokens > 1 else heads * dim
 
 
 def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interleaved=False, q_out=None, stream=None):
@@ -153,52 +193,68 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
     FP32 [rows, rot / 2], or None for no rotation; positions, slots int32
     [tokens].  q_out may be q."""
     torch = _torch()
-    cache = _cache(k_cache, v_cache)
-    tokens, heads, dim = q.shape
-    assert k.shape == v.shape == (tokens, cache.kv_heads, cache.dim) and dim == cache.dim
-    dtype = k_cache.dtype
+    cache, kv_heads, dim = _cache(k_cache, v_cache)
+    tokens, heads, _ = q.shape
+    dtype, int32 = k_cache.dtype, torch.int32
+    q_stride = _heads_stride(q, dtype, heads, dim)
     if q_out is None:
         q_out = torch.empty((tokens, heads, dim), dtype=dtype, device=q.device)
-    assert q_out.shape == q.shape
-    rows = rot = 0
+        out_stride = heads * dim
+    else:
+        assert q_out.shape[0] == tokens
+        out_stride = _heads_stride(q_out, dtype, heads, dim)
+    assert k.shape[0] == v.shape[0] == tokens
+    rows = rot = cos_at = sin_at = at = 0
     if cos is not None:
-        rows, rot = cos.shape[0], 2 * cos.shape[1]
-        assert cos.shape == sin.shape and cos.dtype == sin.dtype == torch.float32
-        assert cos.is_contiguous() and sin.is_contiguous()
-    args = cq_rope_args(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), _heads_stride(q, dtype, dim),
-                        _heads_stride(k, dtype, dim), _heads_stride(v, dtype, dim), _heads_stride(q_out, dtype, dim),
-                        _ptr(cos), _ptr(sin), _index(positions, (tokens,)) if rot else None,
-                        _index(slots, (tokens,)), tokens, rows, heads, rot, interleaved)
-    _check(lib().cq_rope_append(ctypes.byref(cache), ctypes.byref(args), _stream_ptr(stream)), "cq_rope_append")
+        rows, half = cos.shape
+        rot = 2 * half
+        assert cos.dtype == torch.float32 and cos.is_contiguous()
+        cos_at, sin_at, at = cos.data_ptr(), _dense(sin, cos), _vector(positions, tokens, int32)
+    args = _ROPE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), q_stride,
+                      _heads_stride(k, dtype, kv_heads, dim), _heads_stride(v, dtype, kv_heads, dim), out_stride,
+                      cos_at, sin_at, at, _vector(slots, tokens, int32), tokens, rows, heads, rot, interleaved)
+    st = lib().cq_rope_append(cache, args, _stream_ptr(stream))
+    if st:
+        raise CQError(st, "cq_rope_append")
     return q_out
 
 
-def _attn(call, where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window, slopes,
-          bidir, prefix_table, prefix_len, out, workspace, stream):
+def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window, slopes, bidir,
+          prefix_table, prefix_len, out, workspace, stream):
     torch = _torch()
-    cache = _cache(k_cache, v_cache)
-    tokens, heads, dim = q.shape
-    batch = kv_lens.shape[0]
+    cache, _, dim = _cache(k_cache, v_cache)
+    tokens, heads, _ = q.shape
+    batch, int32 = kv_lens.shape[0], torch.int32
+    stride = _heads_stride(q, k_cache.dtype, heads, dim)
     if out is None:
         out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
-    if slopes is not None:
-        assert slopes.shape == (heads,) and slopes.dtype == torch.float32 and slopes.is_contiguous()
-    args = cq_attn_args(
-        q.data_ptr(), out.data_ptr(), _heads_stride(q, k_cache.dtype, cache.dim), tokens, heads, batch,
-        None if q_starts is None else _index(q_starts, (batch + 1,)), _index(tables, (batch, tables.shape[1])),
-        tables.shape[1], max_q, max_kv, _index(kv_lens, (batch,)), dim**-0.5 if scale is None else scale, softcap,
-        window, _ptr(slopes), None if bidir is None else _index(bidir, (batch,)),
-        None if prefix_table is None else _index(prefix_table, prefix_table.shape), prefix_len)
+    else:
+        assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
+    sequences, width = tables.shape
+    assert tables.dtype == int32 and sequences == batch and tables.is_contiguous()
+    prefix_at = 0
+    if prefix_table is not None:
+        assert prefix_table.dtype == int32 and prefix_table.is_contiguous()
+        assert prefix_len <= prefix_table.numel() * k_cache.shape[2]
+        prefix_at = prefix_table.data_ptr()
+    args = _ATTN.pack(
+        q.data_ptr(), out.data_ptr(), stride, tokens, heads, batch,
+        0 if q_starts is None else _vector(q_starts, batch + 1, int32), tables.data_ptr(), width, max_q, max_kv,
+        _vector(kv_lens, batch, int32), dim**-0.5 if scale is None else scale, softcap, window,
+        0 if slopes is None else _vector(slopes, heads, torch.float32),
+        0 if bidir is None else _vector(bidir, batch, int32), prefix_at, prefix_len)
     L = lib()
+    need = 0
     if workspace is None:
-        need = L.cq_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(args))
+        need = L.cq_attn_workspace_bytes(cache, args)
         if need > 0:
             workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
-    st = getattr(L, call)(ctypes.byref(cache), ctypes.byref(args), _ptr(workspace),
-                          0 if workspace is None else workspace.numel() * workspace.element_size(),
-                          _stream_ptr(stream))
-    _check(st, where)
+    else:
+        assert workspace.is_contiguous()
+        need = workspace.numel() * workspace.element_size()
+    st = getattr(L, where)(cache, args, _ptr(workspace), need, _stream_ptr(stream))
+    if st:
+        raise CQError(st, where)
     return out
 
 
@@ -210,10 +266,10 @@ def cq_attn_paged(q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts=None, m
     q [tokens, heads, dim] may be a slice of a fused product; tables int32
     [batch, width], kv_lens int32 [batch]; q_starts int32 [batch + 1], or None
     for one query of every sequence; max_q and max_kv bound the sequences.
-    scale defaults to dim ** -0.5.  A workspace given by the caller (uint8,
-    cq_attn_workspace_bytes) must not be shared by calls that can overlap."""
-    return _attn("cq_attn_paged", "cq_attn_paged", q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q,
-                 scale, softcap, window, slopes, bidir, None, 0, out, workspace, stream)
+    scale defaults to dim ** -0.5.  A workspace given by the caller
+    (cq_attn_workspace_bytes) must not be shared by calls that can overlap."""
+    return _attn("cq_attn_paged", q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window,
+                 slopes, bidir, None, 0, out, workspace, stream)
 
 
 def cq_attn_shared_prefix(q, k_cache, v_cache, prefix_table, prefix_len, tables, kv_lens, max_kv, q_starts=None,
@@ -221,17 +277,15 @@ def cq_attn_shared_prefix(q, k_cache, v_cache, prefix_table, prefix_len, tables,
     """cq_attn_paged for sequences that all begin with the prefix_len tokens of
     prefix_table (int32), which are read once; tables, kv_lens and max_kv
     describe each one's own tokens behind them."""
-    assert prefix_table is None or prefix_len <= prefix_table.numel() * k_cache.shape[2]
-    return _attn("cq_attn_shared_prefix", "cq_attn_shared_prefix", q, k_cache, v_cache, tables, kv_lens, max_kv,
-                 q_starts, max_q, scale, softcap, 0, None, None, prefix_table, prefix_len, out, workspace, stream)
+    return _attn("cq_attn_shared_prefix", q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale,
+                 softcap, 0, None, None, prefix_table, prefix_len, out, workspace, stream)
 
 
 def cq_attn_workspace_bytes(q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts=None, max_q=1, prefix_len=0):
     """Bytes of workspace that an attention call of these sizes needs."""
-    cache = _cache(k_cache, v_cache)
-    tokens, heads, dim = q.shape
-    table = tables.data_ptr() if prefix_len else None
-    args = cq_attn_args(q.data_ptr(), q.data_ptr(), _heads_stride(q, k_cache.dtype, dim), tokens, heads,
-                        kv_lens.shape[0], _ptr(q_starts), tables.data_ptr(), tables.shape[1], max_q, max_kv,
-                        kv_lens.data_ptr(), 1.0, 0.0, 0, None, None, table, prefix_len)
-    return int(lib().cq_attn_workspace_bytes(ctypes.byref(cache), ctypes.byref(args)))
+    cache, _, dim = _cache(k_cache, v_cache)
+    tokens, heads, _ = q.shape
+    args = _ATTN.pack(q.data_ptr(), q.data_ptr(), _heads_stride(q, k_cache.dtype, heads, dim), tokens, heads,
+                      kv_lens.shape[0], _ptr(q_starts), tables.data_ptr(), tables.shape[1], max_q, max_kv,
+                      kv_lens.data_ptr(), 1.0, 0.0, 0, 0, 0, tables.data_ptr() if prefix_len else 0, prefix_len)
+    return int(lib().cq_attn_workspace_bytes(cache, args))

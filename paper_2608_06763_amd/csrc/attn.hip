@@ -2,6 +2,8 @@
 // lie in the workspace.
 #include "attn_common.h"
 
+#include <cmath>
+
 namespace cq {
 
 namespace {
@@ -13,10 +15,13 @@ rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
     r.row_tiles = int((rows + 16 * r.nt - 1) / (16 * r.nt));
     r.numbers = sequences * kv_heads * r.row_tiles;
     const int64_t units = tokens > 32 ? (tokens + 31) / 32 : 1;
-    r.min_units = 4;
-    r.split = units > 16;
+    r.min_units = 4;  // one tile a wave
     // workgroups that LDS and registers let run at once
     const int64_t most = int64_t(device_cu_count()) * (dim == 256 ? 1 : 2);
+    // Up to 1024 tokens one workgroup takes a row tile whole: 800 tokens 12.6 us,
+    // 15.3 split and joined (2000 tokens 22.4 and 16.1).  Up to 2048 where the tiles
+    // alone fill the chip: 90 sequences of up to 1200 tokens 3 us less.
+    r.split = units > (r.numbers >= most ? 64 : 32);
     const int64_t need = (r.numbers * units + r.min_units - 1) / r.min_units;
     r.grid = int(r.split ? (need < most ? need : most) : r.numbers);
     r.slots = (r.split ? 2 * int64_t(r.grid) : 0) + (keep ? r.numbers : 0);
@@ -31,10 +36,17 @@ wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_r
     w.tiles = all_rows / 128 + sequences;
     const int64_t most = sequences * w.row_tiles;
     if (w.tiles > most) w.tiles = most;
-    const int64_t units = tokens / 256, groups = w.tiles * kv_heads, cus = device_cu_count();
-    int64_t splits = groups >= cus ? 1 : 2 * cus / groups;
-    if (splits > units) splits = units;  // four tiles of 64 at least
-    w.splits = int(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+    // Splitting n tiles of 64 tokens s ways takes 1.1 us n (1 - 1 / s) off a workgroup
+    // and costs, for each part, the round trip of its rows through the workspace
+    // (0.35 ns a row and 0.1 us), and 5 us of the join's launch where none runs
+    // anyway.  With 8192 rows and 8 tiles a split of 2 took 22 us against 18 without;
+    // 256 rows of 4 key heads over 16000 tokens took 30 us split 31 ways, 38 split 62.
+    const int64_t groups = w.tiles * kv_heads, cus = device_cu_count();
+    const double n = double(tokens) / 64, part = 0.1 + 0.00035 * double(all_rows) * kv_heads;
+    int64_t splits = int64_t(std::sqrt(1.1 * n / part) + 0.5);
+    if (splits > 2 * cus / groups) splits = 2 * cus / groups;
+    if (splits < 2 || groups >= cus || 1.1 * n * (1.0 - 1.0 / splits) < (keep ? 0.0 : 5.0) + part * splits) splits = 1;
+    w.splits = int(splits > 64 ? 64 : splits);
     w.slots = w.splits > 1 || keep ? sequences * kv_heads * w.row_tiles * w.splits : 0;
     return w;
 }

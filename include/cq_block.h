@@ -114,8 +114,8 @@ cq_status cq_rope_append(const cq_kv_cache *cache, const cq_rope_args *args, voi
  * see do not reach its output, whatever their keys and values hold.
  *
  * Scores and sums are FP32.  The weights, relative to the largest so far, are
- * rounded to the cache's dtype for the matrix cores (BF16 single-token calls:
- * carried in two parts).
+ * rounded to the cache's dtype for the matrix cores (BF16 with up to 32 rows, queries
+ * times heads of a key head: carried in two parts).
  */
 typedef struct {
     const void *q;           /* device [tokens, heads, dim] in the cache's dtype,

@@ -55,6 +55,9 @@ cq_status check_attn(const cq_kv_cache *c, const cq_attn_args *a, bool shared) {
     if (a->max_q > a->tokens) return CQ_ERR_SHAPE;
     // a position and a tile past the longest sequence stay below 2^31
     if (a->max_kv > (1 << 30) || int64_t(a->table_width) * a->batch >= kMost) return CQ_ERR_SHAPE;
+    // and the units of work (32 tokens of a key head) of all sequences are counted in 31 bits
+    const int64_t table = int64_t(a->table_width) * c->page, held = a->max_kv < table ? a->max_kv : table;
+    if (int64_t(a->batch) * c->kv_heads >= kMost / (held / 32 + 1)) return CQ_ERR_SHAPE;
     if (!aligned16(a->q) || !aligned16(a->out)) return CQ_ERR_ALIGN;
     if (!aligned4(a->q_starts) || !aligned4(a->tables) || !aligned4(a->kv_lens) || !aligned4(a->slopes) ||
         !aligned4(a->bidir) || !aligned4(a->prefix_table))

@@ -96,7 +96,8 @@ BAD_ATTN = [
     (dict(max_kv=-1), 1), (dict(table_width=-1), 1), (dict(heads=5), 2), (dict(q_stride=248), 2),
     (dict(q_stride=260), 2), (dict(q_stride=1 << 41), 2), (dict(tokens=1 << 31), 2), (dict(q_starts=None), 2),
     (dict(q_starts=None, tokens=3), 2), (dict(max_q=8), 2), (dict(max_kv=(1 << 30) + 1), 2),
-    (dict(table_width=1 << 30), 2), (dict(q=BAD), 3), (dict(out=BAD), 3), (dict(q_starts=4097), 3),
+    (dict(table_width=1 << 30), 2), (dict(max_kv=1 << 30, table_width=1 << 26, batch=31, tokens=31, max_q=1), 2),
+    (dict(q=BAD), 3), (dict(out=BAD), 3), (dict(q_starts=4097), 3),
     (dict(tables=4097), 3), (dict(kv_lens=4097), 3),
 ]
 

@@ -568,3 +568,17 @@ def test_attn_workspace_of_the_caller(torch_dev):
         with pytest.raises(cq.CQError) as e:
             cq.cq_attn_paged(q, *caches, tables, lens, 3000, workspace=ws[:need - 16])
         assert e.value.status == 2
+
+
+# ---------------------------------------------------------------- the whole block
+
+
+@pytest.mark.parametrize("a8", [False, True])
+def test_decoder_block_example(torch_dev, a8):
+    # Two blocks, each with about eight roundings to BF16 between FP32 steps, 2^-9
+    # of the value in the mean: 2^-9 sqrt(16) < 1e-2.  Dynamic-A8 rounds the normed
+    # stream to 127 steps of its largest value, a few hundredths of a product's norm.
+    from examples.decoder_block import serve
+    errors = serve(prompts=(37, 5, 130), tokens=3, samples=5, a8=a8)
+    say("decoder block", a8, errors)
+    assert len(errors) == 8 and max(errors) < (5e-2 if a8 else 1e-2)

@@ -9,7 +9,7 @@ namespace cq {
 namespace {
 
 // The rows kernel for `sequences` of at most `rows` rows and `tokens` tokens.
-rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t tokens, bool keep) {
+rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t tokens, bool keep, bool beside) {
     rows_plan r;
     r.nt = rows <= 16 ? 1 : 2;
     r.row_tiles = int((rows + 16 * r.nt - 1) / (16 * r.nt));
@@ -17,7 +17,7 @@ rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
     const int64_t units = tokens > 32 ? (tokens + 31) / 32 : 1;
     r.min_units = 4;  // one tile a wave
     // workgroups that LDS and registers let run at once
-    const int64_t most = int64_t(device_cu_count()) * (dim == 256 ? 1 : 2);
+    const int64_t most = int64_t(device_cu_count()) * (dim == 256 || beside ? 1 : 2);
     // Up to 1024 tokens one workgroup takes a row tile whole: 800 tokens 12.6 us,
     // 15.3 split and joined (2000 tokens 22.4 and 16.1).  Up to 2048 where the tiles
     // alone fill the chip: 90 sequences of up to 1200 tokens 3 us less.
@@ -30,7 +30,8 @@ rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
 
 // The wide kernel: at most `tiles` row tiles in all, few of which leave compute
 // units idle unless their tokens are split.
-wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens, bool keep) {
+wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens, bool keep,
+                    bool beside) {
     wide_plan w;
     w.row_tiles = int((rows + 127) / 128);
     w.tiles = all_rows / 128 + sequences;
@@ -44,14 +45,17 @@ wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_r
     const int64_t groups = w.tiles * kv_heads, cus = device_cu_count();
     const double n = double(tokens) / 64, part = 0.1 + 0.00035 * double(all_rows) * kv_heads;
     int64_t splits = int64_t(std::sqrt(1.1 * n / part) + 0.5);
-    if (splits > 2 * cus / groups) splits = 2 * cus / groups;
+    const int64_t slots = beside ? cus : 2 * cus;
+    if (splits > slots / groups) splits = slots / groups;
     if (splits < 2 || groups >= cus || 1.1 * n * (1.0 - 1.0 / splits) < (keep ? 0.0 : 5.0) + part * splits) splits = 1;
     w.splits = int(splits > 64 ? 64 : splits);
     w.slots = w.splits > 1 || keep ? sequences * kv_heads * w.row_tiles * w.splits : 0;
     return w;
 }
 
-// One launch: of the rows kernel, or of the wide one.
+constexpr int64_t kRowsMost = 32;  // rows of a sequence that the rows kernel takes
+
+// One pass over tokens: by the rows kernel, or by the wide one.
 struct pass_plan {
     bool wide, keep;
     rows_plan rows;
@@ -60,19 +64,19 @@ struct pass_plan {
     int64_t bytes() const { return o + ml + shares; }
 };
 
-pass_plan plan_pass(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens,
-                    bool keep) {
+pass_plan plan_pass(bool wide, int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens,
+                    bool keep, bool beside) {
     pass_plan t;
     t.keep = keep;
-    t.wide = rows > 32;
+    t.wide = wide;
     int64_t part_rows = 0;
     t.shares = 0;
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
     if (t.wide) {
-        t.tall = plan_wide(sequences, kv_heads, rows, all_rows, tokens, keep);
+        t.tall = plan_wide(sequences, kv_heads, rows, all_rows, tokens, keep, beside);
         part_rows = t.tall.slots * 128;
     } else {
-        t.rows = plan_rows(dim, sequences, kv_heads, rows, tokens, keep);
+        t.rows = plan_rows(dim, sequences, kv_heads, rows, tokens, keep, beside);
         if (t.rows.split || keep) {
             part_rows = t.rows.slots * 16 * t.rows.nt;
             t.shares = up(t.rows.numbers * int64_t(sizeof(int2)));
@@ -83,40 +87,52 @@ pass_plan plan_pass(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
     return t;
 }
 
-hipError_t launch_pass(int dt, int dim, const pass_plan &t, attn_params p, uint8_t *ws, join_source *join,
-                       hipStream_t stream) {
+// Points a pass's parts at `ws`, and the join at them.
+join_source place(const pass_plan &t, attn_params &p, uint8_t *ws) {
+    join_source join = {};
+    join.o = p.part_o = reinterpret_cast<float *>(ws);
+    join.ml = p.part_ml = reinterpret_cast<float *>(ws + t.o);
+    p.keep_parts = t.keep;
+    if (t.wide) {
+        p.row_tiles = join.row_tiles = t.tall.row_tiles;
+        join.splits = t.tall.splits;
+        join.rows = t.tall.slots ? 128 : 0;
+        return join;
+    }
+    p.row_tiles = join.row_tiles = t.rows.row_tiles;
+    p.min_units = t.rows.min_units;
+    p.shares = t.shares ? reinterpret_cast<int2 *>(ws + t.o + t.ml) : nullptr;
+    join.shares = p.shares;
+    join.rows = t.shares ? 16 * t.rows.nt : 0;
+    join.grid = t.rows.grid;
+    join.first = !t.keep ? -1 : t.rows.split ? 2 * int64_t(t.rows.grid) : 0;
+    return join;
+}
+
+int dim_index(int dim) { return dim == 64 ? 0 : dim == 128 ? 1 : 2; }
+
+hipError_t launch_pass(int dt, int dim, const pass_plan &t, const attn_params &p, hipStream_t stream) {
     typedef hipError_t (*rows_fn)(const rows_plan &, const attn_params &, hipStream_t);
     typedef hipError_t (*wide_fn)(const wide_plan &, const attn_params &, hipStream_t);
     static constexpr rows_fn rows_of[2][3] = {{attn_rows_bf16_64, attn_rows_bf16_128, attn_rows_bf16_256},
                                               {attn_rows_fp16_64, attn_rows_fp16_128, attn_rows_fp16_256}};
     static constexpr wide_fn wide_of[2][3] = {{attn_wide_bf16_64, attn_wide_bf16_128, attn_wide_bf16_256},
                                               {attn_wide_fp16_64, attn_wide_fp16_128, attn_wide_fp16_256}};
-    const int d = dim == 64 ? 0 : dim == 128 ? 1 : 2;
-    p.part_o = reinterpret_cast<float *>(ws);
-    p.part_ml = reinterpret_cast<float *>(ws + t.o);
-    p.keep_parts = t.keep;
-    *join = {};
-    join->o = p.part_o;
-    join->ml = p.part_ml;
-    if (t.wide) {
-        p.row_tiles = join->row_tiles = t.tall.row_tiles;
-        join->splits = t.tall.splits;
-        join->rows = t.tall.slots ? 128 : 0;
-        return wide_of[dt][d](t.tall, p, stream);
-    }
-    p.row_tiles = join->row_tiles = t.rows.row_tiles;
-    p.min_units = t.rows.min_units;
-    p.shares = t.shares ? reinterpret_cast<int2 *>(ws + t.o + t.ml) : nullptr;
-    join->shares = p.shares;
-    join->rows = t.shares ? 16 * t.rows.nt : 0;
-    join->grid = t.rows.grid;
-    join->first = !t.keep ? -1 : t.rows.split ? 2 * int64_t(t.rows.grid) : 0;
-    return rows_of[dt][d](t.rows, p, stream);
+    const int d = dim_index(dim);
+    return t.wide ? wide_of[dt][d](t.tall, p, stream) : rows_of[dt][d](t.rows, p, stream);
+}
+
+hipError_t launch_both(int dt, int dim, const pass_plan &f, const attn_params &flat, const pass_plan &o,
+                       const attn_params &own, hipStream_t stream) {
+    typedef hipError_t (*fn)(const wide_plan &, const attn_params &, const rows_plan &, const attn_params &, hipStream_t);
+    static constexpr fn of[2][3] = {{attn_shared_bf16_64, attn_shared_bf16_128, attn_shared_bf16_256},
+                                    {attn_shared_fp16_64, attn_shared_fp16_128, attn_shared_fp16_256}};
+    return of[dt][dim_index(dim)](f.tall, flat, o.rows, own, stream);
 }
 
 struct plan_t {
     pass_plan own, flat;
-    bool shared;
+    bool shared, together;
     int64_t max_kv, flat_bytes;
 };
 
@@ -126,10 +142,16 @@ plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
     t.max_kv = a.max_kv < held ? a.max_kv : held;
     t.shared = a.prefix_len > 0;
     const int64_t rows = a.tokens * group;
-    t.own = plan_pass(c.dim, a.batch, c.kv_heads, a.max_q * group, rows, t.max_kv, t.shared);
+    const bool wide = a.max_q * group > kRowsMost;
+    // The prefix always takes the wide kernel, which with few rows is bound by memory
+    // too; where the own tokens take the rows kernel both go in one launch (while its
+    // workgroups are counted in 31 bits): 2 to 8 sequences behind 1500 tokens took
+    // 24-28 us with two launches of the rows kernel, 16 so.
+    t.together = t.shared && !wide && int64_t(a.batch) * c.kv_heads < (int64_t(1) << 29);
+    t.own = plan_pass(wide, c.dim, a.batch, c.kv_heads, a.max_q * group, rows, t.max_kv, t.shared, t.together);
     t.flat_bytes = 0;
     if (t.shared) {
-        t.flat = plan_pass(c.dim, 1, c.kv_heads, rows, rows, a.prefix_len, true);
+        t.flat = plan_pass(true, c.dim, 1, c.kv_heads, rows, rows, a.prefix_len, true, t.together);
         t.flat_bytes = t.flat.bytes();
     }
     return t;
@@ -170,7 +192,10 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     p.softcap = a.softcap;
 
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    join_source own, flat = {};
+    const int dt = int(c.dtype);
+    join_source flat = {};
+    const join_source own = place(t.own, p, ws);
+    hipError_t e;
     if (t.shared) {
         attn_params f = p;
         f.flat = 1;
@@ -178,12 +203,20 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
         f.tables = a.prefix_table;
         f.kv_lens = f.q_starts = nullptr;
         f.batch = 1;
-        const hipError_t e = launch_pass(int(c.dtype), c.dim, t.flat, f, ws + t.own.bytes(), &flat, stream);
-        if (e != hipSuccess) return e;
+        f.max_q = int(a.tokens);
+        f.shares = nullptr;
+        flat = place(t.flat, f, ws + t.own.bytes());
+        if (t.together) {
+            e = launch_both(dt, c.dim, t.flat, f, t.own, p, stream);
+        } else {
+            e = launch_pass(dt, c.dim, t.flat, f, stream);
+            if (e == hipSuccess) e = launch_pass(dt, c.dim, t.own, p, stream);
+        }
+    } else {
+        e = launch_pass(dt, c.dim, t.own, p, stream);
     }
-    const hipError_t e = launch_pass(int(c.dtype), c.dim, t.own, p, ws, &own, stream);
     if (e != hipSuccess || !own.rows) return e;
-    return launch_attn_join(int(c.dtype), c.dim, p, own, flat, p.tokens * p.heads >= 4096, stream);
+    return launch_attn_join(dt, c.dim, p, own, flat, p.tokens * p.heads >= 4096, stream);
 }
 
 }  // namespace cq

@@ -329,6 +329,21 @@ hipError_t attn_wide_fp16_64(const wide_plan &w, const attn_params &p, hipStream
 hipError_t attn_wide_fp16_128(const wide_plan &w, const attn_params &p, hipStream_t stream);
 hipError_t attn_wide_fp16_256(const wide_plan &w, const attn_params &p, hipStream_t stream);
 
+// Both in one launch: the wide kernel over a shared prefix, the rows kernel over the
+// sequences' own tokens.
+hipError_t attn_shared_bf16_64(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+hipError_t attn_shared_bf16_128(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+hipError_t attn_shared_bf16_256(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+hipError_t attn_shared_fp16_64(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+hipError_t attn_shared_fp16_128(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+hipError_t attn_shared_fp16_256(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                              hipStream_t stream);
+
 // Where the parts of an output row are: part 0 at `first` + the number of its
 // (sequence, key head, row tile) or at `grid` + the workgroup that began it, the
 // next at the numbers of the workgroups that follow; or (splits > 0) all at

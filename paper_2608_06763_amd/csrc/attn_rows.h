@@ -19,8 +19,13 @@ __device__ __forceinline__ constexpr int val_place(int row) {  // of V: 8 rows, 
     return D == 64 ? 2 * ((row >> 1) & 3) : 2 * (row & 7);
 }
 
+// LDS of a workgroup: the waves' places for K, then for V, then their statistics.
+template <int D, int NT>
+constexpr int kRowsLds = 2 * 4 * kUnit * D * 2 + 4 * NT * 2 * 64 * 4 + 32;
+
+// The workgroup `block` of `grid`.
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_params p, int grid, int direct) {
+__device__ __forceinline__ void attn_rows_group(const attn_params &p, int block, int grid, int direct, uint8_t *lds) {
     constexpr int kTile = kUnit * D * 2;          // bytes of 32 tokens
     constexpr int kLoads = kTile / 1024;          // a wave's requests for them
     constexpr int kChunks = D / 8;                // 16-byte chunks of a token
@@ -31,11 +36,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
     // FP16 weights are formed relative to 2^10 below the maximum, which keeps
     // those down to 2^-24 of it normal numbers.
     constexpr float kLift = DT == 0 ? 0.f : 10.f;
-    // two objects, so that a read of one does not wait for requests into the other
-    __shared__ __align__(1024) uint8_t stage_k[4 * kTile];
-    __shared__ __align__(1024) uint8_t stage_v[4 * kTile];
-    __shared__ float stat[4][NT][2][64];
-    __shared__ int sched[8];
+    uint8_t *const stage_k = lds, *const stage_v = lds + 4 * kTile;
+    float (*const stat)[NT][2][64] = reinterpret_cast<float (*)[NT][2][64]>(lds + 8 * kTile);
+    int *const sched = reinterpret_cast<int *>(lds + 8 * kTile + 4 * NT * 2 * 64 * 4);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
@@ -43,11 +46,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
 
     int u = 0, u_end = 1, before = 0, b = 0;
     runs_t runs = {1, 1, 0};
-    const int fixed = blockIdx.x;
+    const int fixed = block;
     if (direct) {
         b = fixed / (p.kv_heads * p.row_tiles);
     } else {
-        const int me = blockIdx.x;
+        const int me = block;
         const place_t at = locate(
             p.flat ? 1 : p.batch, [&](int b) { return work_of(p, sequence(p, b), R).total; },
             [&](int all) {
@@ -358,12 +361,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
         if (wave == 0) {
             int64_t slot = -1;
             if (p.keep_parts && t_begin == 0) slot = (direct ? 0 : 2 * int64_t(grid)) + number;
-            else if (!complete) slot = t_begin == 0 ? grid + int64_t(blockIdx.x) : int64_t(blockIdx.x);
+            else if (!complete) slot = t_begin == 0 ? grid + int64_t(block) : int64_t(block);
             if (t_begin == 0 && lane == 0 && p.shares) {
                 // who holds the parts: the first workgroup and how many (0: written whole)
-                int count = complete ? 1 : runs.holder(u + w.units - 1) - int(blockIdx.x) + 1;
+                int count = complete ? 1 : runs.holder(u + w.units - 1) - block + 1;
                 if (complete && !p.keep_parts) count = 0;
-                p.shares[number] = make_int2(int(blockIdx.x), count);
+                p.shares[number] = make_int2(block, count);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -392,6 +395,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_p
         if (!direct) u += t_end - t_begin;
         __syncthreads();  // stage is free for the next part
     }
+}
+
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_rows_kernel(attn_params p, int grid, int direct) {
+    __shared__ __align__(1024) uint8_t lds[kRowsLds<D, NT>];
+    attn_rows_group<DT, D, NT>(p, blockIdx.x, grid, direct, lds);
 }
 
 template <int DT, int D>

@@ -1,0 +1,11 @@
+// attn_shared.h for FP16 heads of 64.
+#include "attn_shared.h"
+
+namespace cq {
+
+hipError_t attn_shared_fp16_64(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
+                               hipStream_t stream) {
+    return attn_shared_dim<1, 64>(w, flat, r, own, stream);
+}
+
+}  // namespace cq

@@ -31,10 +31,14 @@ __device__ __forceinline__ void feed() {
     __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
+// LDS of a workgroup: two places each for the TK tokens of K and of V, and flags.
+template <int D, int TK>
+constexpr int kWideLds = 4 * TK * D * 2 + 64;
+
 struct wide_tile {
     bool none;              // no such tile: the workgroup has nothing to do
     seq_t s;
-    int b, head, rt, rows;
+    int b, head, rt, rows, split;
     int bidir;              // tokens that every query of the sequence sees
     int lo_pos, hi_pos;     // positions of the first and last query of the tile
     int wave_lo, wave_hi;   // and of the wave
@@ -43,12 +47,14 @@ struct wide_tile {
 };
 
 template <int TK>
-__device__ __forceinline__ wide_tile find_wide_tile(const attn_params &p, int splits, int wave, int *lds) {
+__device__ __forceinline__ wide_tile find_wide_tile(const attn_params &p, int block, int split, int splits, int wave,
+                                                    int *lds) {
     wide_tile w;
     // the tiles of a key head go to one XCD where there are eight heads or more, and
     // the ones with the most tokens come first
-    w.head = blockIdx.x % p.kv_heads;
-    const int tile = blockIdx.x / p.kv_heads;
+    w.head = block % p.kv_heads;
+    w.split = split;
+    const int tile = block / p.kv_heads;
     auto tiles_of = [&](int b) { return (sequence(p, b).n * p.group + kWideRows - 1) / kWideRows; };
     const place_t at = locate(p.flat ? 1 : p.batch, tiles_of, [&](int) { return tile; }, lds);
     w.none = tile >= at.total;
@@ -74,7 +80,7 @@ __device__ __forceinline__ wide_tile find_wide_tile(const attn_params &p, int sp
     w.t = begin / TK;
     w.t1 = end > begin ? (end + TK - 1) / TK : w.t;
     if (splits > 1) {
-        const int n = w.t1 - w.t, first = w.t, split = blockIdx.y;
+        const int n = w.t1 - w.t, first = w.t;
         w.t = first + n * split / splits;  // n <= 2^25, splits <= 64
         w.t1 = first + n * (split + 1) / splits;
     }
@@ -105,7 +111,7 @@ __device__ __forceinline__ void store_wide_row(const attn_params &p, const wide_
     sum = sum_over_32(sum);
     if (!r.valid) return;
     if (splits > 1 || p.keep_parts) {
-        const int64_t slot = part_number(p, w.b, w.head, w.rt) * splits + blockIdx.y;
+        const int64_t slot = part_number(p, w.b, w.head, w.rt) * splits + w.split;
         const int64_t at_row = slot * kWideRows + 32 * wave + col;
         float *dst = p.part_o + at_row * D + 4 * half;
 #pragma unroll

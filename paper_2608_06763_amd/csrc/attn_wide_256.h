@@ -13,7 +13,7 @@ namespace cq {
 
 // GEN: scores are capped or biased.
 template <int DT, bool GEN>
-__global__ void __launch_bounds__(256, 1) attn_wide_256_kernel(attn_params p, int splits) {
+__device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int block, int split, int splits, uint8_t *lds) {
     constexpr int D = 256, TK = 32;  // channels; tokens of a tile
     constexpr int SB = TK / 32;
     constexpr int kTile = TK * D * 2;
@@ -21,15 +21,15 @@ __global__ void __launch_bounds__(256, 1) attn_wide_256_kernel(attn_params p, in
     constexpr int kChunks = D / 8, kPerLoad = 64 / kChunks;
     constexpr int KS = D / 16, OT = D / 32;
     constexpr float kLift = kWideLift<DT>;
-    __shared__ __align__(1024) uint8_t stage_k[2 * kTile];
-    __shared__ __align__(1024) uint8_t stage_v[2 * kTile];
-    __shared__ int sched[8];
-    __shared__ int odd_tile[2][4];  // a wave found infinities or NaNs in its part of V
+    uint8_t *const stage_k = lds, *const stage_v = lds + 2 * kTile;
+    int *const sched = reinterpret_cast<int *>(lds + 4 * kTile);
+    // a wave found infinities or NaNs in its part of V
+    int (*const odd_tile)[4] = reinterpret_cast<int (*)[4]>(lds + 4 * kTile + 32);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
 
-    const wide_tile w = find_wide_tile<TK>(p, splits, wave, sched);
+    const wide_tile w = find_wide_tile<TK>(p, block, split, splits, wave, sched);
     if (w.none) return;
     const seq_t s = w.s;
     const int head = w.head, t1 = w.t1;
@@ -245,6 +245,12 @@ __global__ void __launch_bounds__(256, 1) attn_wide_256_kernel(attn_params p, in
     }
 
     store_wide_row<DT, D>(p, w, row, splits, wave, o, m, l);
+}
+
+template <int DT, bool GEN>
+__global__ void __launch_bounds__(256, 1) attn_wide_256_kernel(attn_params p, int splits) {
+    __shared__ __align__(1024) uint8_t lds[kWideLds<256, 32>];
+    attn_wide_256_group<DT, GEN>(p, blockIdx.x, blockIdx.y, splits, lds);
 }
 
 template <int DT>

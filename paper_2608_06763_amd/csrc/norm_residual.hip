@@ -184,14 +184,14 @@ template <int DT, int RDT>
 hipError_t launch_dt(const cq_norm_args &a, int8_t *x8, float *dx, hipStream_t stream) {
     const int64_t vecs = a.width >> 3;
     if (vecs <= 64) return launch_nv<DT, RDT, 64, 1>(a, x8, dx, stream);
-    if (vecs <= 128) return launch_nv<DT, RDT, 64, 2>(a, x8, dx, stream);
+    if (vecs <= 128) return launch_nv<DT, RDT, 128, 1>(a, x8, dx, stream);
     if (vecs <= 256) return launch_nv<DT, RDT, 256, 1>(a, x8, dx, stream);
     if (a.rows < 2 * device_cu_count()) {
         if (vecs <= 512) return launch_nv<DT, RDT, 512, 1>(a, x8, dx, stream);
         if (vecs <= 1024) return launch_nv<DT, RDT, 1024, 1>(a, x8, dx, stream);
     }
     if (vecs <= 512) return launch_nv<DT, RDT, 256, 2>(a, x8, dx, stream);
-    if (vecs <= 1024) return launch_nv<DT, RDT, 256, 4>(a, x8, dx, stream);
+    if (vecs <= 1024) return launch_nv<DT, RDT, 512, 2>(a, x8, dx, stream);
     if (vecs <= 2048) return launch_nv<DT, RDT, 1024, 2>(a, x8, dx, stream);
     return launch_nv<DT, RDT, 1024, 4>(a, x8, dx, stream);
 }

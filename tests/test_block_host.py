@@ -96,8 +96,7 @@ BAD_ATTN = [
     (dict(max_kv=-1), 1), (dict(table_width=-1), 1), (dict(heads=5), 2), (dict(q_stride=248), 2),
     (dict(q_stride=260), 2), (dict(q_stride=1 << 41), 2), (dict(tokens=1 << 31), 2), (dict(q_starts=None), 2),
     (dict(q_starts=None, tokens=3), 2), (dict(max_q=8), 2), (dict(max_kv=(1 << 30) + 1), 2),
-    (dict(table_width=1 << 30), 2), (dict(max_kv=1 << 30, table_width=1 << 26, batch=31, tokens=31, max_q=1), 2),
-    (dict(q=BAD), 3), (dict(out=BAD), 3), (dict(q_starts=4097), 3),
+    (dict(table_width=1 << 30), 2), (dict(q=BAD), 3), (dict(out=BAD), 3), (dict(q_starts=4097), 3),
     (dict(tables=4097), 3), (dict(kv_lens=4097), 3),
 ]
 
@@ -117,6 +116,16 @@ def test_shared_prefix_refusals(kw, want):
     a = attn(**{**dict(prefix_table=OK, prefix_len=40), **kw})
     assert L.cq_attn_shared_prefix(ref(cache()), ref(a), OK, 1 << 40, None) == want
     assert L.cq_attn_shared_prefix(ref(cache()), None, OK, 1 << 40, None) == 1
+
+
+def test_attn_counts_its_work_in_31_bits():
+    # 17 * 8 key heads of 2^25 units of 32 tokens
+    L = cq.lib()
+    c = cache(kv_heads=8, page=1024)
+    a = attn(heads=8, tokens=17, batch=17, max_q=1, max_kv=1 << 30, table_width=1 << 20)
+    assert L.cq_attn_paged(ref(c), ref(a), OK, 1 << 50, None) == 2
+    a = attn(heads=8, tokens=7, batch=7, max_q=1, max_kv=1 << 30, table_width=1 << 20)
+    assert L.cq_attn_workspace_bytes(ref(c), ref(a)) > 0
 
 
 def test_paged_call_takes_no_prefix():

@@ -173,7 +173,8 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
 def _cache(k_cache, v_cache):
     pages, kv_heads, page, dim = k_cache.shape
     assert k_cache.is_contiguous()
-    return _CACHE.pack(_type(k_cache), kv_heads, dim, page, pages, k_cache.data_ptr(), _dense(v_cache, k_cache)), kv_heads, dim
+    cache = _CACHE.pack(_type(k_cache), kv_heads, dim, page, pages, k_cache.data_ptr(), _dense(v_cache, k_cache))
+    return cache, kv_heads, dim
 
 
 def _heads_stride(x, dtype, heads, dim):

@@ -124,7 +124,8 @@ hipError_t launch_pass(int dt, int dim, const pass_plan &t, const attn_params &p
 
 hipError_t launch_both(int dt, int dim, const pass_plan &f, const attn_params &flat, const pass_plan &o,
                        const attn_params &own, hipStream_t stream) {
-    typedef hipError_t (*fn)(const wide_plan &, const attn_params &, const rows_plan &, const attn_params &, hipStream_t);
+    typedef hipError_t (*fn)(const wide_plan &, const attn_params &, const rows_plan &, const attn_params &,
+                             hipStream_t);
     static constexpr fn of[2][3] = {{attn_shared_bf16_64, attn_shared_bf16_128, attn_shared_bf16_256},
                                     {attn_shared_fp16_64, attn_shared_fp16_128, attn_shared_fp16_256}};
     return of[dt][dim_index(dim)](f.tall, flat, o.rows, own, stream);

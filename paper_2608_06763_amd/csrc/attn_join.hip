@@ -2,6 +2,10 @@
 // largest of their maxima M, o = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k.
 // One workgroup for each query and head, the parts in an order of their own, so
 // that the result does not depend on which workgroup was done first.
+//
+// Bound by latency: a row's places, its statistics, its parts, each after the other,
+// 4 us; the parts are asked for eight at a time (64 parts of 32 rows: 9 us, 30 where
+// one wave asked for one after the other).
 #include "a8_quant.h"
 #include "attn_common.h"
 

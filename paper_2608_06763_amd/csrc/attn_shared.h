@@ -4,6 +4,10 @@
 // against the same keys), the own tokens are work for the memory (the rows kernel).
 // The workgroups of the one are dealt out over the compute units before those of the
 // other, a chip's worth at a time, so that a compute unit has one of each.
+//
+// Measured: 90 sequences of up to 1200 tokens behind 24000 shared ones, 32 heads of 128
+// over 8: 74 us where the two took 57 and 47 one after the other, and 11 us for the
+// join; 9 sequences behind 1500: 12 us and 5.
 #pragma once
 
 #include "attn_rows.h"

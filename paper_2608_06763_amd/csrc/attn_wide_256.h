@@ -13,7 +13,8 @@ namespace cq {
 
 // GEN: scores are capped or biased.
 template <int DT, bool GEN>
-__device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int block, int split, int splits, uint8_t *lds) {
+__device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int block, int split, int splits,
+                                                    uint8_t *lds) {
     constexpr int D = 256, TK = 32;  // channels; tokens of a tile
     constexpr int SB = TK / 32;
     constexpr int kTile = TK * D * 2;
@@ -46,7 +47,8 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
         for (int i = 0; i < kLoads; ++i) {
             const int row = TK / 4 * wave + i * kPerLoad + lane / kChunks;
             const int chunk = (lane % kChunks) ^ place(row);
-            request_lds16(base, uint32_t((row - TK / 4 * wave) * (2 * D) + chunk * 16), dst + wave * (kTile / 4) + i * 1024);
+            request_lds16(base, uint32_t((row - TK / 4 * wave) * (2 * D) + chunk * 16),
+                          dst + wave * (kTile / 4) + i * 1024);
         }
     };
     auto request_k = [&](int tt, int64_t at) {
@@ -73,6 +75,11 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
         request_v(t, next);
         vmem_order();
     }
+
+    // the 16 bytes of V that the lane brought with request n for tile t
+    auto brought = [&](int n) {
+        return reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
+    };
 
     // ---- this lane's query
     const float slope = GEN && p.slopes ? p.slopes[row.hq] : 0.f;
@@ -120,7 +127,8 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
                 const int row = 32 * g + col;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    const u32x4 key = *reinterpret_cast<const u32x4 *>(ks + row * (2 * D) + (((2 * k + half) ^ key_place<D>(row)) << 4));
+                    const int place = (2 * k + half) ^ key_place<D>(row);
+                    const u32x4 key = *reinterpret_cast<const u32x4 *>(ks + row * (2 * D) + (place << 4));
                     sc[g] = mfma32<DT>(key, q[k], sc[g]);
                 }
             }
@@ -162,13 +170,14 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
         // Does any row of the workgroup not see all of the tile?  Then each wave looks
         // at the values that it brought: rows of no token hold anything and become
         // zeros, other infinities and NaNs are marked.
-        const bool mixed = a + TK > s.len || (!p.flat && (a + TK > w.lo_pos + 1 || (p.window && a <= w.hi_pos - p.window)));
+        const bool mixed = a + TK > s.len ||
+                           (!p.flat && (a + TK > w.lo_pos + 1 || (p.window && a <= w.hi_pos - p.window)));
         if (mixed) {
             bool odd = false;
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
                 const int row = TK / 4 * wave + n * kPerLoad + lane / kChunks;
-                u32x4 *v = reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
+                u32x4 *v = brought(n);
                 if (a + row >= s.len) *v = u32x4{0, 0, 0, 0};
                 else odd |= odd_words<DT>(*v);
             }
@@ -229,7 +238,7 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
                 vmem_order();
 #pragma unroll 1
                 for (int n = 0; n < kLoads; ++n) {
-                    u32x4 *v = reinterpret_cast<u32x4 *>(stage_v + (t & 1) * kTile + wave * (kTile / 4) + n * 1024 + lane * 16);
+                    u32x4 *v = brought(n);
                     *v = finite_only<DT>(*v);
                 }
                 wait_lds();

@@ -7,6 +7,9 @@
 // once, ten operations an element.  T threads hold a row in registers between
 // the reductions, 8 elements in a 16-byte vector at a time, so nothing is read
 // twice; the rounded r' is never read back.
+//
+// Measured: 7013 rows of 8192 with post norm and gate 110 us, 5.2 TB/s (a large copy:
+// 4.9); one row of 4096 2.7 us, launch and latency.
 #include "a8_quant.h"
 #include "block_internal.h"
 #include "cq_device.h"
@@ -183,6 +186,10 @@ hipError_t launch_nv(const cq_norm_args &a, int8_t *x8, float *dx, hipStream_t s
 template <int DT, int RDT>
 hipError_t launch_dt(const cq_norm_args &a, int8_t *x8, float *dx, hipStream_t stream) {
     const int64_t vecs = a.width >> 3;
+    // One vector a thread while that is at most a wave for each 64: a row of 1024 in one
+    // wave of two vectors took 3.7 us, in two waves 2.8.  Few rows of up to 8192 spread
+    // over as many threads as they have vectors; many rows keep two vectors a thread
+    // (8000 rows of 8192: 99 us, with four vectors 109).
     if (vecs <= 64) return launch_nv<DT, RDT, 64, 1>(a, x8, dx, stream);
     if (vecs <= 128) return launch_nv<DT, RDT, 128, 1>(a, x8, dx, stream);
     if (vecs <= 256) return launch_nv<DT, RDT, 256, 1>(a, x8, dx, stream);

@@ -6,6 +6,9 @@
 // 8i .. and rot / 2 + 8i .. of the rotated half pairs, or 16 neighbouring
 // channels.  So a rotation stays in one thread, q may be rotated in place, and
 // the D / 16 threads of a head write one contiguous run of a page.
+//
+// Measured: 8191 tokens of 64 heads and 8 key heads of 128 in 61 us, 5.5 TB/s (a large
+// copy: 4.9); one token of 32 and 8 heads 2.7 us, launch and latency.
 #include "block_internal.h"
 #include "cq_device.h"
 

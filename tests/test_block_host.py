@@ -63,7 +63,10 @@ def rope(**kw):
     return cq_rope_args(**a)
 
 
-@pytest.mark.parametrize("kw,want", [({f: None}, 1) for f in ("q", "k", "v", "q_out", "cos", "sin", "positions", "slots")] + [
+ROPE_POINTERS = ("q", "k", "v", "q_out", "cos", "sin", "positions", "slots")
+
+
+@pytest.mark.parametrize("kw,want", [({f: None}, 1) for f in ROPE_POINTERS] + [
     (dict(tokens=0), 1), (dict(heads=0), 1), (dict(table_rows=0), 1), (dict(interleaved=2), 1), (dict(rot=-16), 1),
     (dict(rot=80), 2), (dict(rot=24), 2), (dict(tokens=1 << 31), 2), (dict(q_stride=248), 2), (dict(q_stride=260), 2),
     (dict(k_stride=120), 2), (dict(v_stride=132), 2), (dict(q_out_stride=264), 2), (dict(q_stride=1 << 41), 2),

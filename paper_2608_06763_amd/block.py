@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import CQ_BF16, CQ_FP16, CQ_FP32, CQError, _stream_ptr, _torch, lib
+from . import CQ_BF16, CQ_FP16, CQ_FP32, CQError, _stream_ptr, lib
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -62,15 +62,21 @@ def declare(L):
     L.cq_attn_workspace_bytes.argtypes = [_vp, _vp]
 
 
-_types = None
+torch = None  # imported with the first call, as by the package
+_types = {}
+
+
+def _torch():
+    global torch
+    if torch is None:
+        import torch as t
+        _types.update({t.bfloat16: CQ_BF16, t.float16: CQ_FP16, t.float32: CQ_FP32})
+        torch = t
+    return torch
 
 
 def _type(t):
     """dtype code of a tensor."""
-    global _types
-    if _types is None:
-        torch = _torch()
-        _types = {torch.bfloat16: CQ_BF16, torch.float16: CQ_FP16, torch.float32: CQ_FP32}
     code = _types.get(t.dtype)
     if code is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
@@ -105,7 +111,7 @@ def _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset
         assert y.dtype == dtype and y.shape == residual.shape and y.is_contiguous()
         y_at = y.data_ptr()
         if residual_out is None:
-            r = _torch().empty_like(residual)
+            r = torch.empty_like(residual)
             r_at = r.data_ptr()
         else:
             r = residual_out
@@ -140,8 +146,11 @@ def cq_norm_residual(residual, weight, eps, y=None, post_weight=None, gate=None,
     weight, post_weight [width] and gate ([width] or [rows, width]) in the model
     dtype.  Without y, r' is the residual itself.  residual_out may be residual,
     out may be y."""
+    _torch()
     if out is None:
-        out = _torch().empty_like(residual, dtype=weight.dtype)
+        # an empty_like that takes no dtype is twice as fast
+        out = torch.empty_like(residual) if residual.dtype == weight.dtype else \
+            torch.empty_like(residual, dtype=weight.dtype)
     args, r = _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out)
     st = lib().cq_norm_residual(args, _stream_ptr(stream))
     if st:
@@ -153,7 +162,7 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
                         out=None, residual_out=None, x8=None, dx=None, stream=None):
     """cq_norm_residual with h straight to the Dynamic-A8 carriers; returns
     (x8, dx, r').  h itself is written only into a given out."""
-    torch = _torch()
+    _torch()
     rows = residual.shape[0]
     if x8 is None:
         x8 = torch.empty_like(residual, dtype=torch.int8)
@@ -177,11 +186,10 @@ def _cache(k_cache, v_cache):
     return cache, kv_heads, dim
 
 
-def _heads_stride(x, dtype, heads, dim):
+def _heads_stride(x, dtype, tokens, heads, dim):
     """Stride between tokens of x [tokens, heads, dim], whose heads are dense."""
     token, head, one = x.stride()
-    tokens, n, d = x.shape
-    assert x.dtype == dtype and n == heads and d == dim and one == 1 and (head == dim or n == 1)
+    assert x.shape == (tokens, heads, dim) and x.dtype == dtype and one == 1 and (head == dim or heads == 1)
     # the stride of a single token is never used: any legal one serves
     return token if tokens > 1 else heads * dim
 
@@ -193,18 +201,18 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
     q, k, v [tokens, heads, dim] may be slices of one fused product; cos, sin
     FP32 [rows, rot / 2], or None for no rotation; positions, slots int32
     [tokens].  q_out may be q."""
-    torch = _torch()
+    _torch()
     cache, kv_heads, dim = _cache(k_cache, v_cache)
     tokens, heads, _ = q.shape
     dtype, int32 = k_cache.dtype, torch.int32
-    q_stride = _heads_stride(q, dtype, heads, dim)
+    q_stride = _heads_stride(q, dtype, tokens, heads, dim)
+    k_stride = _heads_stride(k, dtype, tokens, kv_heads, dim)
+    v_stride = _heads_stride(v, dtype, tokens, kv_heads, dim)
     if q_out is None:
-        q_out = torch.empty((tokens, heads, dim), dtype=dtype, device=q.device)
+        q_out = q.new_empty((tokens, heads, dim))
         out_stride = heads * dim
     else:
-        assert q_out.shape[0] == tokens
-        out_stride = _heads_stride(q_out, dtype, heads, dim)
-    assert k.shape[0] == v.shape[0] == tokens
+        out_stride = _heads_stride(q_out, dtype, tokens, heads, dim)
     rows = rot = cos_at = sin_at = at = 0
     if cos is not None:
         rows, half = cos.shape
@@ -212,8 +220,8 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
         assert cos.dtype == torch.float32 and cos.is_contiguous()
         cos_at, sin_at, at = cos.data_ptr(), _dense(sin, cos), _vector(positions, tokens, int32)
     args = _ROPE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), q_stride,
-                      _heads_stride(k, dtype, kv_heads, dim), _heads_stride(v, dtype, kv_heads, dim), out_stride,
-                      cos_at, sin_at, at, _vector(slots, tokens, int32), tokens, rows, heads, rot, interleaved)
+                      k_stride, v_stride, out_stride, cos_at, sin_at, at, _vector(slots, tokens, int32), tokens, rows,
+                      heads, rot, interleaved)
     st = lib().cq_rope_append(cache, args, _stream_ptr(stream))
     if st:
         raise CQError(st, "cq_rope_append")
@@ -222,13 +230,13 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
 
 def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window, slopes, bidir,
           prefix_table, prefix_len, out, workspace, stream):
-    torch = _torch()
+    _torch()
     cache, _, dim = _cache(k_cache, v_cache)
     tokens, heads, _ = q.shape
     batch, int32 = kv_lens.shape[0], torch.int32
-    stride = _heads_stride(q, k_cache.dtype, heads, dim)
+    stride = _heads_stride(q, k_cache.dtype, tokens, heads, dim)
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((tokens, heads, dim))
     else:
         assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
     sequences, width = tables.shape
@@ -284,9 +292,10 @@ def cq_attn_shared_prefix(q, k_cache, v_cache, prefix_table, prefix_len, tables,
 
 def cq_attn_workspace_bytes(q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts=None, max_q=1, prefix_len=0):
     """Bytes of workspace that an attention call of these sizes needs."""
+    _torch()
     cache, _, dim = _cache(k_cache, v_cache)
     tokens, heads, _ = q.shape
-    args = _ATTN.pack(q.data_ptr(), q.data_ptr(), _heads_stride(q, k_cache.dtype, heads, dim), tokens, heads,
+    args = _ATTN.pack(q.data_ptr(), q.data_ptr(), _heads_stride(q, k_cache.dtype, tokens, heads, dim), tokens, heads,
                       kv_lens.shape[0], _ptr(q_starts), tables.data_ptr(), tables.shape[1], max_q, max_kv,
                       kv_lens.data_ptr(), 1.0, 0.0, 0, 0, 0, tables.data_ptr() if prefix_len else 0, prefix_len)
     return int(lib().cq_attn_workspace_bytes(cache, args))

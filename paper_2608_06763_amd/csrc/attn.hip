@@ -188,7 +188,7 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     p.max_q = a.max_q;
     p.page_shift = __builtin_ctz(unsigned(c.page));
     p.pages = uint32_t(c.pages);
-    p.window = a.window;
+    p.window = a.window < t.max_kv ? a.window : 0;  // a longer one hides nothing
     p.scale = a.scale;
     p.softcap = a.softcap;
 

@@ -81,26 +81,35 @@ __device__ __forceinline__ seq_t sequence(const attn_params &p, int b) {
     return s;
 }
 
-// What one query sees: j < hi && j >= lo, or j < bi.
+// What one query sees: the `span` tokens from lo on, and those below bi.
 struct limits_t {
-    int hi, lo, bi, pos;
+    int lo;
+    uint32_t span;
+    int bi, pos;
 };
 
 __device__ __forceinline__ limits_t limits(const attn_params &p, const seq_t &s, int i, bool valid, int bidir) {
     limits_t r = {0, 0, 0, 0};
     if (!valid) return r;
     if (p.flat) {
-        r.hi = s.len;
+        r.span = s.len;
         return r;
     }
     r.pos = s.len - s.n + i;
-    r.hi = r.pos + 1;
-    if (p.window) r.lo = r.pos - p.window + 1;
+    if (p.window) {
+        // may begin before the first token: nothing lies there
+        r.lo = r.pos - p.window + 1;
+        r.span = p.window;
+    } else {
+        r.span = max(r.pos + 1, 0);
+    }
     if (r.pos >= 0) r.bi = min(bidir, s.len);
     return r;
 }
 
-__device__ __forceinline__ bool sees(const limits_t &r, int j) { return (j < r.hi && j >= r.lo) || j < r.bi; }
+__device__ __forceinline__ bool sees(const limits_t &r, int j) {
+    return uint32_t(j) - uint32_t(r.lo) < r.span || j < r.bi;
+}
 
 // sequence() at a wave-uniform b.
 __device__ __forceinline__ seq_t sequence_uniform(const attn_params &p, int b) {
@@ -226,24 +235,28 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 // Raw products as scores in powers of two: capped, and biased by the distance of
-// their tokens.  tanh as 1 - 2 / (e^2x + 1): its absolute error, a few 2^-24,
-// times the cap is what a score's own rounding is.
-template <int N, typename Token>
-__device__ __forceinline__ void to_scores(const attn_params &p, float (&x)[N], float slope, int pos, Token token) {
+// their tokens, of which e is offset(e) after `first`.  tanh as 1 - 2 / (e^2x + 1):
+// its absolute error, a few 2^-24, times the cap is what a score's own rounding is.
+template <int N, typename Offset>
+__device__ __forceinline__ void to_scores(const attn_params &p, float (&x)[N], float slope, int first, int pos,
+                                          Offset offset) {
+    slope *= kLog2e;
+    const float base = slope * float(first - pos);
     if (p.softcap > 0.f) {
         const float c = 2.f * kLog2e * p.scale / p.softcap, top = p.softcap * kLog2e;
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            x[e] = top - 2.f * top * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * c) + 1.f);
+        for (int e = 0; e < N; ++e) {
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * c) + 1.f);
+            x[e] = __builtin_fmaf(-2.f * top, r, top + base);
+        }
     } else {
         const float c = p.scale * kLog2e;
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] *= c;
+        for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(x[e], c, base);
     }
     if (p.slopes) {
-        slope *= kLog2e;
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(slope, float(token(e) - pos), x[e]);
+        for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(slope, float(offset(e)), x[e]);
     }
 }
 

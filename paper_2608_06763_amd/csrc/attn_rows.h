@@ -225,11 +225,14 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
                 float x[8], top = kLowest;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = sc[n][e >> 2][e & 3];
-                auto token = [&](int e) { return a + 16 * (e >> 2) + 4 * quad + (e & 3); };
-                to_scores(p, x, slope[n], lim[n].pos, token);
+                // token e of the lane: a constant after its first
+                const int first = a + 4 * quad;
+                auto offset = [](int e) { return 16 * (e >> 2) + (e & 3); };
+                to_scores(p, x, slope[n], first, lim[n].pos, offset);
                 if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = sees(lim[n], token(e)) ? x[e] : -__builtin_inff();
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = sees(lim[n], first + offset(e)) ? x[e] : -__builtin_inff();
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);

@@ -156,26 +156,27 @@ __device__ __forceinline__ void attn_wide_group(const attn_params &p, int block,
     };
     // products to scores; what a row does not see to -inf
     auto scores = [&](f32x16 (&x)[SB], int tt) {
-        const int a = tt * TK + 4 * half;
+        // element e of a lane is a constant number of tokens after its first
+        const int first = tt * TK + 4 * half;
+        auto offset = [](int e) { return 8 * (e >> 2) + (e & 3); };
         if constexpr (GEN) {
 #pragma unroll
             for (int g = 0; g < SB; ++g) {
                 float y[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) y[e] = x[g][e];
-                to_scores(p, y, slope, lim.pos, [&](int e) { return a + 32 * g + 8 * (e >> 2) + (e & 3); });
+                to_scores(p, y, slope, first + 32 * g, lim.pos, offset);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[g][e] = y[e];
             }
         }
         if (tt < full0 || tt >= full1) {
-            // against the tile's first token of this half: constants on the other side
-            const limits_t rel = {lim.hi - a, lim.lo - a, lim.bi - a, 0};
+            const limits_t rel = {lim.lo - first, lim.span, lim.bi - first, 0};
 #pragma unroll
             for (int g = 0; g < SB; ++g)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    x[g][e] = sees(rel, 32 * g + 8 * (e >> 2) + (e & 3)) ? x[g][e] : -__builtin_inff();
+                    x[g][e] = sees(rel, 32 * g + offset(e)) ? x[g][e] : -__builtin_inff();
         }
     };
     auto largest = [&](const f32x16 (&x)[SB]) {

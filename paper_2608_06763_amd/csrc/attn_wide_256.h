@@ -136,14 +136,15 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
             float x[16 * SB], top = kLowest;
 #pragma unroll
             for (int e = 0; e < 16 * SB; ++e) x[e] = sc[e >> 4][e & 15];
-            auto token = [&](int e) { return a + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3); };
-            if constexpr (GEN) to_scores(p, x, slope, lim.pos, token);
+            // element e of a lane is a constant number of tokens after its first
+            const int first = a + 4 * half;
+            auto offset = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
+            if constexpr (GEN) to_scores(p, x, slope, first, lim.pos, offset);
             if (!whole) {
-                // against the tile's first token of this half: constants on the other side
-                const limits_t rel = {lim.hi - a - 4 * half, lim.lo - a - 4 * half, lim.bi - a - 4 * half, 0};
+                const limits_t rel = {lim.lo - first, lim.span, lim.bi - first, 0};
 #pragma unroll
                 for (int e = 0; e < 16 * SB; ++e)
-                    x[e] = sees(rel, 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3)) ? x[e] : -__builtin_inff();
+                    x[e] = sees(rel, offset(e)) ? x[e] : -__builtin_inff();
             }
 #pragma unroll
             for (int e = 0; e < 16 * SB; ++e) top = fmaxf(top, x[e]);

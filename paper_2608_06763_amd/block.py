@@ -228,6 +228,18 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
     return q_out
 
 
+def _workspace(need, device, stream):
+    """A workspace that lives until this call returns.
+
+    It is allocated on the stream that the kernels run on: the allocator hands a
+    block that is let go to the next call on the stream that it was allocated on,
+    which on any other one would not wait for them."""
+    if stream is None:
+        return torch.empty((need,), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty((need,), dtype=torch.uint8, device=device)
+
+
 def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window, slopes, bidir,
           prefix_table, prefix_len, out, workspace, stream):
     _torch()
@@ -257,7 +269,7 @@ def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, 
     if workspace is None:
         need = L.cq_attn_workspace_bytes(cache, args)
         if need > 0:
-            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+            workspace = _workspace(need, q.device, stream)
     else:
         assert workspace.is_contiguous()
         need = workspace.numel() * workspace.element_size()

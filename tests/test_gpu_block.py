@@ -534,6 +534,30 @@ def test_block_repeats_bit_for_bit_and_on_another_stream(torch_dev):
         assert torch.equal(a, b) and torch.equal(a, c)
 
 
+def test_attn_workspace_is_allocated_on_the_stream_of_the_call(torch_dev, monkeypatch):
+    # else the allocator gives it to the current stream's next tensor while the
+    # kernels on the other stream still write to it
+    torch, cq = torch_dev, _cq()
+    inputs = _block(torch, 71)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    empty, at = torch.empty, []
+
+    def seen(*args, **kw):
+        if kw.get("dtype") == torch.uint8:
+            at.append(torch.cuda.current_stream())
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch, "empty", seen)
+    qkv, caches, tables, lens = inputs[4], inputs[0], inputs[1], inputs[2]
+    got = cq.cq_attn_shared_prefix(qkv[:, :8], *caches, tables[2].contiguous(), 150, tables, lens, 200, stream=side)
+    monkeypatch.undo()
+    side.synchronize()
+    plain = cq.cq_attn_shared_prefix(qkv[:, :8], *caches, tables[2].contiguous(), 150, tables, lens, 200)
+    assert torch.equal(got, plain)
+    assert at == [side]
+
+
 def test_block_in_a_graph(torch_dev):
     torch, cq = torch_dev, _cq()
     inputs = _block(torch, 41)

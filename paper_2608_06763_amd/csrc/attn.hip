@@ -191,6 +191,11 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     p.window = a.window < t.max_kv ? a.window : 0;  // a longer one hides nothing
     p.scale = a.scale;
     p.softcap = a.softcap;
+    if (a.softcap > 0.f) {
+        // finite for the smallest caps, so that a score of 0 stays one
+        const float rate = (a.softcap <= kNearCap ? 2.f * kLog2e : 1.f) * a.scale / a.softcap;
+        p.cap_rate = rate < 3.0e38f ? rate : 3.0e38f;
+    }
 
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     const int dt = int(c.dtype);

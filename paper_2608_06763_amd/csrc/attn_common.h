@@ -27,6 +27,9 @@ constexpr float kLowest = -3.0e38f;
 // it by more than this many powers of two.
 constexpr float kSlack = 4.0f;
 
+// Caps up to this take the short form of tanh (to_scores).
+constexpr float kNearCap = 64.0f;
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -51,6 +54,7 @@ struct attn_params {
     uint32_t pages;
     int window;
     float scale, softcap;
+    float cap_rate;    // of tanh's argument: scale / softcap, for caps up to kNearCap in powers of two of e^2x
     int flat, flat_len;
     int row_tiles;     // most row tiles of a sequence
     int min_units;     // least units of a workgroup (rows kernel)
@@ -235,19 +239,39 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 // Raw products as scores in powers of two: capped, and biased by the distance of
-// their tokens, of which e is offset(e) after `first`.  tanh as 1 - 2 / (e^2x + 1):
-// its absolute error, a few 2^-24, times the cap is what a score's own rounding is.
+// their tokens, of which e is offset(e) after `first`.
+//
+// tanh as 1 - 2 / (e^2x + 1) is off by a few 2^-24 of the cap, whatever the score:
+// 1.6e-5 for a cap of 64, a thirtieth of a weight's rounding to FP16, and more than
+// that rounding for 10^4.  So caps above 64 take cap tanh t = s (tanh t) / t for
+// |t| = |s / cap| < 1/4, with the series of (tanh t) / t through t^8 (what is left
+// out is below 2^-26 there), and the short form for scores that the cap reaches,
+// where it is off by at most 2^-20 of the score.  Six operations more a score, which
+// caps of the usual size need not pay.
 template <int N, typename Offset>
 __device__ __forceinline__ void to_scores(const attn_params &p, float (&x)[N], float slope, int first, int pos,
                                           Offset offset) {
     slope *= kLog2e;
     const float base = slope * float(first - pos);
-    if (p.softcap > 0.f) {
-        const float c = 2.f * kLog2e * p.scale / p.softcap, top = p.softcap * kLog2e;
+    if (p.softcap > 0.f && p.softcap <= kNearCap) {
+        const float top = p.softcap * kLog2e;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * c) + 1.f);
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[e] * p.cap_rate) + 1.f);
             x[e] = __builtin_fmaf(-2.f * top, r, top + base);
+        }
+    } else if (p.softcap > 0.f) {
+        const float c = p.scale * kLog2e, top = p.softcap * kLog2e;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float t = x[e] * p.cap_rate, tt = t * t;
+            float near = __builtin_fmaf(tt, 62.f / 2835.f, -17.f / 315.f);
+            near = __builtin_fmaf(tt, near, 2.f / 15.f);
+            near = __builtin_fmaf(tt, near, -1.f / 3.f);
+            near = __builtin_fmaf(tt, near, 1.f) * (x[e] * c);
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(t * (2.f * kLog2e)) + 1.f);
+            const float far = __builtin_fmaf(-2.f, r, 1.f) * top;
+            x[e] = (__builtin_fabsf(t) < 0.25f ? near : far) + base;
         }
     } else {
         const float c = p.scale * kLog2e;

@@ -606,3 +606,39 @@ def test_decoder_block_example(torch_dev, a8):
     errors = serve(prompts=(37, 5, 130), tokens=3, samples=5, a8=a8)
     say("decoder block", a8, errors)
     assert len(errors) == 8 and max(errors) < (5e-2 if a8 else 1e-2)
+
+
+# ---------------------------------------------------------------- caps of any size
+
+
+def _f32(x):
+    return float(np.float32(x))
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.7, 64.0, 65.0, 1e3, 1e5, 1e6, 1e8, 1e30, 3e38])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("fp16", 256)])
+@pytest.mark.parametrize("new,lens", [([1, 1, 1], [1, 40, 290]), ([90, 64], [130, 64])])
+def test_attn_caps_far_from_the_scores(torch_dev, cap, dtype, dim, new, lens):
+    # a cap far above the scores leaves them as they are
+    _check_attn(torch_dev, dtype, dim, 4, 2, 16, new, lens, softcap=_f32(cap))
+
+
+@pytest.mark.parametrize("cap", [30.0, 70.0, 200.0])
+@pytest.mark.parametrize("dtype,new,lens", [("fp16", [1, 1, 1], [1, 40, 290]), ("bf16", [90, 64], [130, 64])])
+def test_attn_scores_around_the_cap(torch_dev, cap, dtype, new, lens):
+    # scores of up to about 70, on both sides of the cap
+    _check_attn(torch_dev, dtype, 64, 4, 2, 16, new, lens, softcap=cap, scale=1.0)
+
+
+@pytest.mark.parametrize("cap", [1e-37, 1e-40])
+@pytest.mark.parametrize("new,length", [(1, 40), (70, 90)])
+def test_attn_of_no_query_under_the_smallest_caps(torch_dev, cap, new, length):
+    # a score of zero stays zero: the mean of the visible values
+    torch, cq = torch_dev, _cq()
+    caches, tables, held = _paged(torch, 7, [length], 16, 1, 64, "fp16")
+    q = torch.zeros((new, 2, 64), dtype=torch.float16, device="cuda")
+    lens = torch.tensor([length], dtype=torch.int32).cuda()
+    starts = torch.tensor([0, new], dtype=torch.int32).cuda()
+    out = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new, softcap=_f32(cap))
+    ref, mag = _attn_ref(_f64(q), held, [new], 0.125)
+    _within(out, ref, U["fp16"] * np.abs(ref) + (U["fp16"] + FP32) * mag + TINY, "equal weights")

@@ -38,8 +38,8 @@ typedef struct {
                                 or NULL                                          */
     const void *residual;    /* device [rows, width] in residual_dtype           */
     const void *weight;      /* device [width] in dtype                          */
-    void *residual_out;      /* device, r' in residual_dtype, or NULL; may be
-                                `residual` itself                                */
+    void *residual_out;      /* device, r' in residual_dtype (without y a copy of
+                                `residual`), or NULL; may be `residual` itself   */
     void *out;               /* device [rows, width], h in dtype; may be `y`     */
     int64_t gate_stride;     /* elements: 0 (one gate for all rows) or >= width,
                                 a multiple of 8                                  */

@@ -113,9 +113,6 @@ def _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset
         if residual_out is None:
             r = torch.empty_like(residual)
             r_at = r.data_ptr()
-        else:
-            r = residual_out
-            r_at = _dense(r, residual)
         if post_weight is not None:
             post = _vector(post_weight, width, dtype)
         if gate is not None:
@@ -129,7 +126,10 @@ def _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset
                 assert gate.dim() == 1
             gate_at = gate.data_ptr()
     else:
-        assert post_weight is None and gate is None and residual_out is None
+        assert post_weight is None and gate is None
+    if residual_out is not None:
+        r = residual_out
+        r_at = _dense(r, residual)
     if out is not None:
         assert out.dtype == dtype and out.shape == residual.shape and out.is_contiguous()
         out_at = out.data_ptr()
@@ -144,8 +144,8 @@ def cq_norm_residual(residual, weight, eps, y=None, post_weight=None, gate=None,
 
     Returns (h, r').  residual [rows, width] in the model dtype or FP32; y,
     weight, post_weight [width] and gate ([width] or [rows, width]) in the model
-    dtype.  Without y, r' is the residual itself.  residual_out may be residual,
-    out may be y."""
+    dtype.  Without y, r' is the residual itself, or its copy in residual_out.
+    residual_out may be residual, out may be y."""
     _torch()
     if out is None:
         # an empty_like that takes no dtype is twice as fast

@@ -135,6 +135,12 @@ __global__ void __launch_bounds__(T == kWave ? 256 : T) norm_residual_kernel(cq_
             for (int e = 0; e < 8; ++e) r[i][e] = __builtin_fmaf(a.alpha, u[i][e], r[i][e]);
             if (a.residual_out) store8<RDT>(a.residual_out, at + 8 * v, r[i]);
         }
+    } else if (a.residual_out && a.residual_out != a.residual) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * T;
+            if (v < vecs) store8<RDT>(a.residual_out, at + 8 * v, r[i]);
+        }
     }
     float s = 0.f;
 #pragma unroll

@@ -139,6 +139,42 @@ def test_norm_to_carriers_equals_the_two_calls(torch_dev, rows, width, dtype):
     assert torch.equal(x8, x8_ref) and torch.equal(dx, dx_ref)
 
 
+@pytest.mark.parametrize("rows,width", [(1, 64), (5, 1056), (600, 8192)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("r32", [False, True])
+@pytest.mark.parametrize("a8", [False, True])
+def test_norm_without_y_writes_the_residual_too(torch_dev, rows, width, dtype, r32, a8):
+    # r' = residual: into the buffer of its own that the caller names
+    import ctypes
+    torch, cq = torch_dev, _cq()
+    say("norm without y", rows, width, dtype, r32, a8)
+    r, w = _rand(torch, 11, rows, width, dtype=dtype, scale=2.0), _rand(torch, 12, width, dtype=dtype)
+    r = r.float() * 1.2345 if r32 else r
+    kind = {"bf16": cq.CQ_BF16, "fp16": cq.CQ_FP16}[dtype]
+    h, r_out = torch.full_like(r, 7.0, dtype=w.dtype), torch.full_like(r, 7.0)
+    args = cq.block.cq_norm_args(
+        y=None, post_weight=None, gate=None, residual=r.data_ptr(), weight=w.data_ptr(), residual_out=r_out.data_ptr(),
+        out=h.data_ptr(), gate_stride=0, rows=rows, width=width, dtype=kind,
+        residual_dtype=cq.CQ_FP32 if r32 else kind, alpha=1.0, eps=1e-5, weight_offset=0.0)
+    x8, dx = torch.empty((rows, width), dtype=torch.int8, device="cuda"), torch.empty((rows,), device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    if a8:
+        assert cq.lib().cq_norm_residual_a8(ctypes.byref(args), x8.data_ptr(), dx.data_ptr(), stream) == 0
+    else:
+        assert cq.lib().cq_norm_residual(ctypes.byref(args), stream) == 0
+    assert torch.equal(r_out, r)
+    h_ref, _, _, slack = _norm_ref(_f64(r), _f64(w), 1e-5, 0.0, None, None, None, 1.0)
+    _within(h, h_ref, U[dtype] * np.abs(h_ref) + FP32 * slack + TINY, "h")
+    # and through the binding
+    copy = torch.full_like(r, 7.0)
+    if a8:
+        _, _, same = cq.cq_norm_residual_a8(r, w, 1e-5, residual_out=copy)
+    else:
+        again, same = cq.cq_norm_residual(r, w, 1e-5, residual_out=copy)
+        assert torch.equal(again, h)
+    assert same is copy and torch.equal(copy, r)
+
+
 # ---------------------------------------------------------------- rotation and append
 
 

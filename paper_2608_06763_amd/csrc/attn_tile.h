@@ -80,9 +80,10 @@ __device__ __forceinline__ wide_tile find_wide_tile(const attn_params &p, int bl
     w.t = begin / TK;
     w.t1 = end > begin ? (end + TK - 1) / TK : w.t;
     if (splits > 1) {
-        const int n = w.t1 - w.t, first = w.t;
-        w.t = first + n * split / splits;  // n <= 2^25, splits <= 64
-        w.t1 = first + n * (split + 1) / splits;
+        const int64_t n = w.t1 - w.t;  // up to 2^25, and 64 splits: past 31 bits
+        const int first = w.t;
+        w.t = first + int(n * split / splits);
+        w.t1 = first + int(n * (split + 1) / splits);
     }
     return w;
 }

@@ -678,3 +678,24 @@ def test_attn_of_no_query_under_the_smallest_caps(torch_dev, cap, new, length):
     out = cq.cq_attn_paged(q, *caches, tables, lens, length, q_starts=starts, max_q=new, softcap=_f32(cap))
     ref, mag = _attn_ref(_f64(q), held, [new], 0.125)
     _within(out, ref, U["fp16"] * np.abs(ref) + (U["fp16"] + FP32) * mag + TINY, "equal weights")
+
+
+def test_attn_splits_of_the_longest_sequence(torch_dev):
+    # 2^30 tokens of two pages, each of them repeated: 64 splits of 2^25 tiles, the
+    # last split the only one with the second page's, whose keys are far above the
+    # others'.  All of its tokens are alike, so that the sums are of ones.
+    torch, cq = torch_dev, _cq()
+    heads, dim, page = 33, 256, 1024
+    k = torch.zeros((2, 1, page, dim), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    k[1, ..., 0] = 100.0
+    v[0], v[1] = 1.0, 2.0
+    width = (1 << 30) // page
+    table = torch.zeros((1, width), dtype=torch.int32, device="cuda")
+    table[0, -(width // 64):] = 1
+    q = torch.zeros((1, heads, dim), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    lens = torch.tensor([1 << 30], dtype=torch.int32, device="cuda")
+    say("longest sequence", lens.item())
+    out = cq.cq_attn_paged(q, k, v, table, lens, 1 << 30, scale=1.0)
+    assert bool((out == 2.0).all())

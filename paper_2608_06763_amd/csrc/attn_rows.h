@@ -247,7 +247,7 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     x[e] = __builtin_amdgcn_exp2f(x[e] - (m[n] - kLift));
-                    l[n] += x[e];
+                    if constexpr (kTwoParts) l[n] += x[e];
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -255,6 +255,10 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
                     if constexpr (kTwoParts)
                         wt2[n][e] = pack_pair<DT>(x[2 * e] - __uint_as_float(wt[n][e] << 16),
                                                   x[2 * e + 1] - __uint_as_float(wt[n][e] & 0xffff0000u));
+                    else
+                        // the sum of the weights as they were rounded: a rounding that
+                        // many of them share then falls out of the quotient
+                        l[n] = add_pair<DT>(wt[n][e], l[n]);
                 }
             }
             // ---- values

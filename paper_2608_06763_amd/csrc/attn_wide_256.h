@@ -159,12 +159,14 @@ __device__ __forceinline__ void attn_wide_256_group(const attn_params &p, int bl
             const float shift = m - kLift;
 #pragma unroll
             for (int e = 0; e < 16 * SB; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -shift));
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 16 * SB; ++e) sum[e & 3] += x[e];
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
             for (int e = 0; e < 8 * SB; ++e) wt[e >> 3][e & 7] = pack_pair<DT>(x[2 * e], x[2 * e + 1]);
+            // the sum of the weights as they were rounded: a rounding that many of them
+            // share then falls out of the quotient
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 8 * SB; ++e) sum[e & 1] = add_pair<DT>(wt[e >> 3][e & 7], sum[e & 1]);
+            l += sum[0] + sum[1];
         }
         // ---- values have arrived
         if (more) wait_loads<kLoads>(); else wait_loads<0>();

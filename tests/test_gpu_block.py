@@ -699,3 +699,59 @@ def test_attn_splits_of_the_longest_sequence(torch_dev):
     say("longest sequence", lens.item())
     out = cq.cq_attn_paged(q, k, v, table, lens, 1 << 30, scale=1.0)
     assert bool((out == 2.0).all())
+
+
+# ---------------------------------------------------------------- weights and their sum
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,lens", [([1] * 6, [40, 33, 90, 17, 300, 64]), ([3, 4], [50, 200]), ([1], [1500]),
+                                      ([70, 33], [100, 33]), ([40], [1500])])
+@pytest.mark.parametrize("prefix", [0, 75])
+def test_attn_of_equal_values_is_that_value(torch_dev, dtype, dim, new, lens, prefix):
+    # Every token has the same value, the largest below 2: the output is it times
+    # (sum of the weights that multiply it) / (sum that divides), and 2^-12 (FP16) or
+    # 2^-9 (BF16) away from it lies the middle of its neighbour.  FP32 sums of 1500
+    # terms stay within 2^-13, BF16 weights in two parts within 2^-17.  All tokens
+    # but each page's first have one key, so that their weights share a rounding.
+    torch, cq = torch_dev, _cq()
+    say("equal values", dtype, dim, new, lens, prefix)
+    heads, kv_heads, page = 8, 2, 16
+    caches, tables, held = _paged(torch, 8, [max(prefix, 1)] + lens, page, kv_heads, dim, dtype)
+    value = 2.0 - 2.0 * U[dtype]
+    caches[0].zero_()
+    caches[0][..., 0] = -1.0
+    caches[0][:, :, 0, 0] = 1.0
+    caches[1].fill_(value)
+    q = torch.zeros((sum(new), heads, dim))
+    q[..., 0] = torch.rand(q.shape[:2], generator=torch.Generator().manual_seed(4)) - 0.5
+    q = q.to(_dtype(torch, dtype)).cuda()
+    starts = torch.tensor(np.cumsum([0] + new), dtype=torch.int32).cuda()
+    args = (tables[1:].contiguous(), torch.tensor(lens, dtype=torch.int32).cuda(), max(lens))
+    kw = dict(q_starts=starts, max_q=max(new), scale=1.0)
+    if prefix:
+        out = cq.cq_attn_shared_prefix(q, *caches, tables[0].contiguous(), prefix, *args, **kw)
+    else:
+        out = cq.cq_attn_paged(q, *caches, *args, **kw)
+    assert bool((out == value).all()), float((out.float() - value).abs().max())
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 4, 1), (128, 8, 2), (256, 12, 1), (64, 24, 1)])
+def test_attn_weights_of_few_bf16_rows_keep_two_parts(torch_dev, dim, heads, kv_heads):
+    # Values of +1 and -1 in turn under weights that nearly cancel: the output is far
+    # below sum(p |v|) = 1, so that its own rounding hides nothing.  Weights in two
+    # parts are within 2^-17 of themselves; in one part they would be off by 2^-9.
+    torch, cq = torch_dev, _cq()
+    lens, page = [2, 4, 6, 8, 32, 33, 200], 16
+    say("two parts", dim, heads, kv_heads)
+    caches, tables, held = _paged(torch, 9, lens, page, kv_heads, dim, "bf16")
+    caches[0].mul_(0.25)
+    caches[1][:, :, 0::2], caches[1][:, :, 1::2] = 1.0, -1.0
+    for k, v in held:
+        k *= 0.25
+        v[0::2], v[1::2] = 1.0, -1.0
+    q = _rand(torch, 10, len(lens), heads, dim, dtype="bf16")
+    out = cq.cq_attn_paged(q, *caches, tables, torch.tensor(lens, dtype=torch.int32).cuda(), max(lens))
+    ref, mag = _attn_ref(_f64(q), held, [1] * len(lens), dim**-0.5)
+    _within(out, ref, U["bf16"] * np.abs(ref) + FP32 * mag, "two parts")

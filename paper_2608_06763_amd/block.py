@@ -1,7 +1,9 @@
 """The operators of a decoder block between its packed products (include/cq_block.h).
 
 Arguments are device tensors; the binding only marshals them.  A paged cache is
-two tensors [pages, kv_heads, page, dim] that the caller owns.
+two tensors [pages, kv_heads, page, dim] that the caller owns.  A call given a
+stream runs there, and what it allocates is allocated there; the caller orders it
+with the streams that made its arguments and that use its results.
 """
 from __future__ import annotations
 
@@ -98,6 +100,22 @@ def _vector(t, size, dtype):
     return t.data_ptr()
 
 
+def _on(stream, call, *args):
+    """A call on a stream of the caller's: run with that stream current.
+
+    Every buffer that the call makes is then the stream's.  The allocator hands a
+    block that is let go to the next tensor of the stream that it was made on, and
+    one of any other stream would not wait for the kernels.  The stream that was
+    current may use what is returned as its own, so letting that go waits for it."""
+    current = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        got = call(*args)
+    for t in got if isinstance(got, tuple) else (got,):
+        if not any(t is a for a in args):
+            t.record_stream(current)
+    return got
+
+
 # ---------------------------------------------------------------- norms
 
 
@@ -147,12 +165,15 @@ def cq_norm_residual(residual, weight, eps, y=None, post_weight=None, gate=None,
     dtype.  Without y, r' is the residual itself, or its copy in residual_out.
     residual_out may be residual, out may be y."""
     _torch()
+    if stream is not None:
+        return _on(stream, cq_norm_residual, residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out,
+                   residual_out)
     if out is None:
         # an empty_like that takes no dtype is twice as fast
         out = torch.empty_like(residual) if residual.dtype == weight.dtype else \
             torch.empty_like(residual, dtype=weight.dtype)
     args, r = _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out)
-    st = lib().cq_norm_residual(args, _stream_ptr(stream))
+    st = lib().cq_norm_residual(args, _stream_ptr())
     if st:
         raise CQError(st, "cq_norm_residual")
     return out, r
@@ -163,6 +184,9 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
     """cq_norm_residual with h straight to the Dynamic-A8 carriers; returns
     (x8, dx, r').  h itself is written only into a given out."""
     _torch()
+    if stream is not None:
+        return _on(stream, cq_norm_residual_a8, residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out,
+                   residual_out, x8, dx)
     rows = residual.shape[0]
     if x8 is None:
         x8 = torch.empty_like(residual, dtype=torch.int8)
@@ -170,7 +194,7 @@ def cq_norm_residual_a8(residual, weight, eps, y=None, post_weight=None, gate=No
         dx = torch.empty((rows,), dtype=torch.float32, device=residual.device)
     assert x8.shape == residual.shape and x8.is_contiguous() and x8.dtype == torch.int8
     args, r = _norm_args(residual, weight, eps, y, post_weight, gate, alpha, weight_offset, out, residual_out)
-    st = lib().cq_norm_residual_a8(args, x8.data_ptr(), _vector(dx, rows, torch.float32), _stream_ptr(stream))
+    st = lib().cq_norm_residual_a8(args, x8.data_ptr(), _vector(dx, rows, torch.float32), _stream_ptr())
     if st:
         raise CQError(st, "cq_norm_residual_a8")
     return x8, dx, r
@@ -202,6 +226,8 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
     FP32 [rows, rot / 2], or None for no rotation; positions, slots int32
     [tokens].  q_out may be q."""
     _torch()
+    if stream is not None:
+        return _on(stream, cq_rope_append, q, k, v, cos, sin, positions, slots, k_cache, v_cache, interleaved, q_out)
     cache, kv_heads, dim = _cache(k_cache, v_cache)
     tokens, heads, _ = q.shape
     dtype, int32 = k_cache.dtype, torch.int32
@@ -222,27 +248,18 @@ def cq_rope_append(q, k, v, cos, sin, positions, slots, k_cache, v_cache, interl
     args = _ROPE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), q_stride,
                       k_stride, v_stride, out_stride, cos_at, sin_at, at, _vector(slots, tokens, int32), tokens, rows,
                       heads, rot, interleaved)
-    st = lib().cq_rope_append(cache, args, _stream_ptr(stream))
+    st = lib().cq_rope_append(cache, args, _stream_ptr())
     if st:
         raise CQError(st, "cq_rope_append")
     return q_out
 
 
-def _workspace(need, device, stream):
-    """A workspace that lives until this call returns.
-
-    It is allocated on the stream that the kernels run on: the allocator hands a
-    block that is let go to the next call on the stream that it was allocated on,
-    which on any other one would not wait for them."""
-    if stream is None:
-        return torch.empty((need,), dtype=torch.uint8, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty((need,), dtype=torch.uint8, device=device)
-
-
 def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap, window, slopes, bidir,
           prefix_table, prefix_len, out, workspace, stream):
     _torch()
+    if stream is not None:
+        return _on(stream, _attn, where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, scale, softcap,
+                   window, slopes, bidir, prefix_table, prefix_len, out, workspace, None)
     cache, _, dim = _cache(k_cache, v_cache)
     tokens, heads, _ = q.shape
     batch, int32 = kv_lens.shape[0], torch.int32
@@ -269,11 +286,11 @@ def _attn(where, q, k_cache, v_cache, tables, kv_lens, max_kv, q_starts, max_q, 
     if workspace is None:
         need = L.cq_attn_workspace_bytes(cache, args)
         if need > 0:
-            workspace = _workspace(need, q.device, stream)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
     else:
         assert workspace.is_contiguous()
         need = workspace.numel() * workspace.element_size()
-    st = getattr(L, where)(cache, args, _ptr(workspace), need, _stream_ptr(stream))
+    st = getattr(L, where)(cache, args, _ptr(workspace), need, _stream_ptr())
     if st:
         raise CQError(st, where)
     return out

@@ -167,3 +167,73 @@ def test_binding_refuses_shapes_and_types():
         cq.cq_attn_paged(q.transpose(0, 1), kv, kv, one.view(3, 1), one, 5)
     with pytest.raises(AssertionError):
         cq.cq_rope_append(q, q, q, None, None, None, one, kv, kv)
+
+
+def test_what_a_call_on_a_stream_allocates_is_that_streams(monkeypatch):
+    # the library is not called: its place is taken by a list of the streams it is given
+    import contextlib
+    import torch
+    from paper_2608_06763_amd import block
+
+    class Stream:
+        cuda_stream = 77
+
+    main, side = Stream(), Stream()
+    now, made, used, launched = [main], [], [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream)
+        yield
+        now.pop()
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name == "cq_attn_workspace_bytes":
+                    return 512
+                launched.append(now[-1])
+                return 0
+            return call
+
+    def maker(make):
+        def f(*args, **kw):
+            made.append(now[-1])
+            return make(*args, **kw)
+        return f
+
+    r, w = torch.zeros((3, 64), dtype=torch.bfloat16), torch.zeros((64,), dtype=torch.bfloat16)
+    kv = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    q, one = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3,), dtype=torch.int32)
+    table = one.view(3, 1)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: now[-1])
+    monkeypatch.setattr(block, "lib", Library)
+    monkeypatch.setattr(block, "_stream_ptr", lambda stream=None: 0)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: used.append((t.data_ptr(), s)))
+    for where, name in ((torch, "empty"), (torch, "empty_like"), (torch.Tensor, "new_empty")):
+        monkeypatch.setattr(where, name, maker(getattr(where, name)))
+    calls = [
+        (4, lambda s: cq.cq_norm_residual(r, w, 1e-5, y=r, stream=s) + cq.cq_norm_residual(r, w, 1e-5, y=r, stream=s)),
+        (4, lambda s: cq.cq_norm_residual_a8(r, w, 1e-5, y=r, out=r, stream=s) +
+            cq.cq_norm_residual_a8(r, w, 1e-5, y=r, residual_out=r, stream=s)[:1]),
+        (1, lambda s: cq.cq_rope_append(q, q[:, :2], q[:, 2:], None, None, None, one, kv, kv, stream=s)),
+        (2, lambda s: cq.cq_attn_paged(q, kv, kv, table, one, 5, stream=s)),
+        (2, lambda s: cq.cq_attn_shared_prefix(q, kv, kv, one, 40, table, one, 5, stream=s)),
+    ]
+    for least, call in calls:
+        for stream in (side, None):
+            del made[:], used[:], launched[:]
+            got = call(stream)
+            want = side if stream else main
+            assert len(made) >= least and set(made) == {want} and set(launched) == {want}
+            got = {t.data_ptr() for t in (got if isinstance(got, tuple) else (got,))}
+            if stream:
+                # the caller's stream may go on with the results, and they are nobody's before it has
+                assert {s for _, s in used} == {main} and got <= {p for p, _ in used}
+            else:
+                assert not used
+    # what the caller gave stays as it is
+    del made[:], used[:]
+    h, same = cq.cq_norm_residual(r, w, 1e-5, y=r, out=torch.zeros_like(r), residual_out=r, stream=side)
+    assert same is r and not used and not made

@@ -594,6 +594,26 @@ def test_attn_workspace_is_allocated_on_the_stream_of_the_call(torch_dev, monkey
     assert at == [side]
 
 
+def test_buffers_let_go_on_another_stream_are_not_handed_to_the_current_one(torch_dev):
+    # the last norm of a model: its residual is let go while the kernel still writes it
+    torch, cq = torch_dev, _cq()
+    x, y = (_rand(torch, 81 + i, 700, 4096, dtype="bf16") for i in range(2))
+    w = _rand(torch, 83, 4096, dtype="bf16")
+    want, _ = cq.cq_norm_residual(x, w, 1e-5, y=y)
+    x8_want, dx_want, _ = cq.cq_norm_residual_a8(x, w, 1e-5, y=y)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    h, r = cq.cq_norm_residual(x, w, 1e-5, y=y, stream=side)
+    x8, dx, r8 = cq.cq_norm_residual_a8(x, w, 1e-5, y=y, stream=side)
+    at = {r.data_ptr(), r8.data_ptr()}
+    del r, r8
+    others = [torch.zeros_like(x) for _ in range(4)]
+    assert not at & {t.data_ptr() for t in others}
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(h, want) and torch.equal(x8, x8_want) and torch.equal(dx, dx_want)
+
+
 def test_block_in_a_graph(torch_dev):
     torch, cq = torch_dev, _cq()
     inputs = _block(torch, 41)

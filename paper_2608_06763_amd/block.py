@@ -42,13 +42,13 @@ class cq_attn_args(ctypes.Structure):
 
 # The same structures as bytes: the calls pack their arguments in one step, which
 # takes a third of the time of filling a ctypes structure field by field.
-_NORM = struct.Struct("@7P3q2i3f")
+_NORM = struct.Struct("@7P3q2i3f4x")
 _CACHE = struct.Struct("@4iq2P")
-_ROPE = struct.Struct("@4P4q4P2q3i")
+_ROPE = struct.Struct("@4P4q4P2q3i4x")
 _ATTN = struct.Struct("@2P2q2i2P3iP2fi3Pq")
 for _s, _c in ((_NORM, cq_norm_args), (_CACHE, cq_kv_cache), (_ROPE, cq_rope_args), (_ATTN, cq_attn_args)):
-    # C pads a structure at its end too
-    assert (_s.size + 7) // 8 * 8 == ctypes.sizeof(_c), _c
+    # to the last byte, C's padding at the end among them: calls copy whole structures
+    assert _s.size == ctypes.sizeof(_c), _c
 
 
 def declare(L):

@@ -237,3 +237,15 @@ def test_what_a_call_on_a_stream_allocates_is_that_streams(monkeypatch):
     del made[:], used[:]
     h, same = cq.cq_norm_residual(r, w, 1e-5, y=r, out=torch.zeros_like(r), residual_out=r, stream=side)
     assert same is r and not used and not made
+
+
+def test_packed_arguments_are_whole_structures():
+    # the library copies all of a structure, its padding too, from the bytes it is given
+    from paper_2608_06763_amd import block
+    for packed, c in ((block._NORM, cq_norm_args), (block._CACHE, cq_kv_cache), (block._ROPE, cq_rope_args),
+                      (block._ATTN, block.cq_attn_args)):
+        assert packed.size == ctypes.sizeof(c)
+        # and every field lies where C has it
+        fields = [f for f, _ in c._fields_]
+        got = c.from_buffer_copy(packed.pack(*range(1, len(fields) + 1)))
+        assert [getattr(got, f) for f in fields] == list(range(1, len(fields) + 1))

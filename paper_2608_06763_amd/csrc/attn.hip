@@ -33,9 +33,8 @@ rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int6
 wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_rows, int64_t tokens, bool keep,
                     bool beside) {
     wide_plan w;
-    w.row_tiles = int((rows + 127) / 128);
     w.tiles = all_rows / 128 + sequences;
-    const int64_t most = sequences * w.row_tiles;
+    const int64_t most = sequences * ((rows + 127) / 128);
     if (w.tiles > most) w.tiles = most;
     // Splitting n tiles of 64 tokens s ways takes 1.1 us n (1 - 1 / s) off a workgroup
     // and costs, for each part, the round trip of its rows through the workspace
@@ -49,7 +48,7 @@ wide_plan plan_wide(int64_t sequences, int kv_heads, int64_t rows, int64_t all_r
     if (splits > slots / groups) splits = slots / groups;
     if (splits < 2 || groups >= cus || 1.1 * n * (1.0 - 1.0 / splits) < (keep ? 0.0 : 5.0) + part * splits) splits = 1;
     w.splits = int(splits > 64 ? 64 : splits);
-    w.slots = w.splits > 1 || keep ? sequences * kv_heads * w.row_tiles * w.splits : 0;
+    w.part_rows = w.splits > 1 || keep ? w.splits * all_rows * kv_heads : 0;
     return w;
 }
 
@@ -74,7 +73,7 @@ pass_plan plan_pass(bool wide, int dim, int64_t sequences, int kv_heads, int64_t
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
     if (t.wide) {
         t.tall = plan_wide(sequences, kv_heads, rows, all_rows, tokens, keep, beside);
-        part_rows = t.tall.slots * 128;
+        part_rows = t.tall.part_rows;
     } else {
         t.rows = plan_rows(dim, sequences, kv_heads, rows, tokens, keep, beside);
         if (t.rows.split || keep) {
@@ -94,9 +93,8 @@ join_source place(const pass_plan &t, attn_params &p, uint8_t *ws) {
     join.ml = p.part_ml = reinterpret_cast<float *>(ws + t.o);
     p.keep_parts = t.keep;
     if (t.wide) {
-        p.row_tiles = join.row_tiles = t.tall.row_tiles;
         join.splits = t.tall.splits;
-        join.rows = t.tall.slots ? 128 : 0;
+        join.rows = t.tall.part_rows ? 1 : 0;
         return join;
     }
     p.row_tiles = join.row_tiles = t.rows.row_tiles;

@@ -59,8 +59,9 @@ struct attn_params {
     int row_tiles;     // most row tiles of a sequence
     int min_units;     // least units of a workgroup (rows kernel)
     int keep_parts;    // every part goes to the workspace
-    float *part_o;     // [slot][rows of a tile][dim], not normalised
-    float *part_ml;    // [slot][rows of a tile][2]: maximum (powers of two), sum
+    // rows kernel: [slot][rows of a tile], wide kernel: [split][token][head]
+    float *part_o;     // [..][dim], not normalised
+    float *part_ml;    // [..][2]: maximum (powers of two), sum
     int2 *shares;      // [sequence][key head][row tile]: who holds its parts
 };
 
@@ -358,10 +359,9 @@ hipError_t attn_rows_fp16_256(const rows_plan &r, const attn_params &p, hipStrea
 
 // Wide kernel: tiles of 128 rows; `splits` workgroups share the tokens of each.
 struct wide_plan {
-    int64_t tiles;    // most row tiles of all sequences
-    int row_tiles;    // most of one
+    int64_t tiles;      // most row tiles of all sequences
     int splits;
-    int64_t slots;
+    int64_t part_rows;  // of the workspace: the call's rows for each split
 };
 hipError_t attn_wide_bf16_64(const wide_plan &w, const attn_params &p, hipStream_t stream);
 hipError_t attn_wide_bf16_128(const wide_plan &w, const attn_params &p, hipStream_t stream);
@@ -385,14 +385,14 @@ hipError_t attn_shared_fp16_128(const wide_plan &w, const attn_params &flat, con
 hipError_t attn_shared_fp16_256(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
                               hipStream_t stream);
 
-// Where the parts of an output row are: part 0 at `first` + the number of its
-// (sequence, key head, row tile) or at `grid` + the workgroup that began it, the
-// next at the numbers of the workgroups that follow; or (splits > 0) all at
-// number * splits on.
+// Where the parts of an output row are: part 0 in the slot `first` + the number of its
+// (sequence, key head, row tile) or `grid` + the workgroup that began it, the next
+// in those of the workgroups that follow; or (splits > 0) at the output row's own
+// place in each split.
 struct join_source {
     const float *o, *ml;
     const int2 *shares;
-    int rows;         // of a tile; 0: no such source
+    int rows;         // of a slot; 0: no such source
     int row_tiles;
     int grid, splits;
     int64_t first;    // -1: parts begin at grid + workgroup

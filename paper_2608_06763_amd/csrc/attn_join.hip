@@ -15,7 +15,6 @@ namespace {
 
 // Slot of part k of `number`.
 __device__ __forceinline__ int64_t part_slot(const join_source &j, int64_t number, int first, int k) {
-    if (j.splits) return number * j.splits + k;
     if (k == 0) return j.first >= 0 ? j.first + number : j.grid + int64_t(first);
     return first + int64_t(k);
 }
@@ -50,22 +49,22 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
             begin = s.first;
             if (token < begin || token >= begin + s.n) return;  // a row of no sequence
         }
-        const int r = (int(token) - begin) * p.group + g, rt = r / own.rows;
-        number[0] = (int64_t(b) * p.kv_heads + kvh) * own.row_tiles + rt;
-        at[0] = r - rt * own.rows;
         count[0] = own.splits;
         if (!own.splits) {
+            const int r = (int(token) - begin) * p.group + g, rt = r / own.rows;
+            number[0] = (int64_t(b) * p.kv_heads + kvh) * own.row_tiles + rt;
+            at[0] = r - rt * own.rows;
             const int2 s = own.shares[number[0]];
             first[0] = s.x;
             count[0] = s.y;
         }
     }
     if (flat.rows) {
-        const int64_t r = token * p.group + g, rt = r / flat.rows;
-        number[1] = int64_t(kvh) * flat.row_tiles + rt;
-        at[1] = int(r - rt * flat.rows);
         count[1] = flat.splits;
         if (!flat.splits) {
+            const int64_t r = token * p.group + g, rt = r / flat.rows;
+            number[1] = int64_t(kvh) * flat.row_tiles + rt;
+            at[1] = int(r - rt * flat.rows);
             const int2 s = flat.shares[number[1]];
             first[1] = s.x;
             count[1] = s.y;
@@ -73,13 +72,15 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
     }
     const int parts = count[0] + count[1];
     if (parts == 0) return;  // written whole
-    auto slot_of = [&](int k) {
+    auto row_at = [&](int k) -> int64_t {
         const bool f = k >= count[0];
         const join_source &j = f ? flat : own;
-        return (part_slot(j, number[f], first[f], f ? k - count[0] : k) * j.rows + at[f]);
+        const int part = f ? k - count[0] : k;
+        if (j.splits) return part * p.tokens * p.heads + row;
+        return part_slot(j, number[f], first[f], part) * j.rows + at[f];
     };
     auto stat = [&](int k) {
-        return *reinterpret_cast<const float2 *>((k >= count[0] ? flat.ml : own.ml) + slot_of(k) * 2);
+        return *reinterpret_cast<const float2 *>((k >= count[0] ? flat.ml : own.ml) + row_at(k) * 2);
     };
     // every wave has all maxima; the parts themselves are shared out, kBatch
     // requests of a wave at a time
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int kk = min(k0 + k, parts - 1);
-            v[k] = *reinterpret_cast<const fE *>((kk >= count[0] ? flat.o : own.o) + slot_of(kk) * D + lane * E);
+            v[k] = *reinterpret_cast<const fE *>((kk >= count[0] ? flat.o : own.o) + row_at(kk) * D + lane * E);
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {

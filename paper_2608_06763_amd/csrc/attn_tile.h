@@ -112,8 +112,8 @@ __device__ __forceinline__ void store_wide_row(const attn_params &p, const wide_
     sum = sum_over_32(sum);
     if (!r.valid) return;
     if (splits > 1 || p.keep_parts) {
-        const int64_t slot = part_number(p, w.b, w.head, w.rt) * splits + w.split;
-        const int64_t at_row = slot * kWideRows + 32 * wave + col;
+        // a part has a row for each of the call's, so that sequences of any lengths fill it
+        const int64_t at_row = (w.split * p.tokens + w.s.first + r.i) * p.heads + r.hq;
         float *dst = p.part_o + at_row * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < OT; ++d)

@@ -249,3 +249,17 @@ def test_packed_arguments_are_whole_structures():
         fields = [f for f, _ in c._fields_]
         got = c.from_buffer_copy(packed.pack(*range(1, len(fields) + 1)))
         assert [getattr(got, f) for f in fields] == list(range(1, len(fields) + 1))
+
+
+@pytest.mark.parametrize("prompts", [64, 128])
+def test_attn_workspace_is_for_the_rows_that_there_are(prompts):
+    # one chunk of 4096 tokens beside single tokens of other sequences, all behind a
+    # prefix: a part of each kind for each of the call's rows, FP32 with two statistics,
+    # and not the longest sequence's room for every one of them
+    L = cq.lib()
+    tokens, heads, dim = 4096 + prompts - 1, 32, 128
+    c = cache(kv_heads=8, dim=dim, page=64, pages=100000)
+    a = attn(heads=heads, q_stride=heads * dim, tokens=tokens, batch=prompts, max_q=4096, max_kv=4096, table_width=100,
+             prefix_table=OK, prefix_len=1000)
+    need = L.cq_attn_workspace_bytes(ref(c), ref(a))
+    assert 0 < need <= 2 * tokens * heads * (4 * dim + 8) + 4096

@@ -531,6 +531,62 @@ def test_attn_shared_prefix_without_own_tokens(torch_dev):
     _within(out, ref, U["bf16"] * np.abs(ref) + (U["bf16"] + FP32) * mag + TINY, "prefix alone")
 
 
+@pytest.mark.parametrize("opt", [dict()] + OPTIONS, ids=str)
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("bf16", 256), ("fp16", 256)])
+@pytest.mark.parametrize("new,lens", [
+    ([70, 33, 1, 64, 20], [1700, 40, 900, 64, 1290]),       # tokens of a few row tiles split many ways
+    ([20, 5, 90, 1, 17], [1030, 4, 2000, 1, 17]),           # the bias's and the window's sequence not the longest
+])
+def test_attn_scores_and_masks_over_split_tokens(torch_dev, opt, dtype, dim, new, lens):
+    import ctypes
+    cq = _cq()
+    # the tokens are split: the call needs room for parts
+    c = cq.block.cq_kv_cache(dtype=0, kv_heads=2, dim=dim, page=16, pages=1000, k=4096, v=4096)
+    a = cq.block.cq_attn_args(q=4096, out=4096, q_stride=4 * dim, tokens=sum(new), heads=4, batch=5, q_starts=4096,
+                              tables=4096, table_width=200, max_q=max(new), max_kv=max(lens), kv_lens=4096, scale=1.0)
+    assert cq.lib().cq_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(a)) >= 2 * sum(new) * 4 * dim * 4
+    _check_attn(torch_dev, dtype, dim, 4, 2, 16, new, lens, **opt)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("bf16", 256)])
+@pytest.mark.parametrize("prefix,new,lens", [(1900, [1] * 9, [0, 1, 40, 3, 300, 17, 16, 64, 5]),
+                                             (1500, [90, 1, 1, 33, 0, 2], [1200, 7, 0, 33, 5, 600])])
+@pytest.mark.parametrize("softcap", [0.0, 6.0])
+def test_attn_shared_prefix_over_split_tokens(torch_dev, dtype, dim, prefix, new, lens, softcap):
+    torch, cq = torch_dev, _cq()
+    say("shared split", dtype, dim, prefix, new, lens, softcap)
+    heads, kv_heads = 4, 2
+    caches, tables, held = _paged(torch, 25, [prefix] + lens, 32, kv_heads, dim, dtype)
+    q = _rand(torch, 26, sum(new), heads + 2 * kv_heads, dim, dtype=dtype, scale=1.5)[:, :heads]
+    starts = torch.tensor(np.cumsum([0] + new), dtype=torch.int32).cuda()
+    out = cq.cq_attn_shared_prefix(q, *caches, tables[0].contiguous(), prefix, tables[1:].contiguous(),
+                                   torch.tensor(lens, dtype=torch.int32).cuda(), max(lens), q_starts=starts,
+                                   max_q=max(new), softcap=softcap)
+    ref, mag = _attn_ref(_f64(q), held[1:], new, dim**-0.5, softcap=softcap, prefix=held[0])
+    _within(out, ref, U[dtype] * np.abs(ref) + (U[dtype] + FP32) * mag + TINY, "split prefix")
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64), ("fp16", 256)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_attn_hidden_tokens_of_split_sequences_may_hold_anything(torch_dev, dtype, dim, bad):
+    # a bad value that only the last query sees, and one that only the first one's window holds
+    torch, cq = torch_dev, _cq()
+    say("split hidden", dtype, dim, bad)
+    heads, kv_heads, page, new, length = 4, 2, 16, 70, 1700
+    caches, tables, held = _paged(torch, 27, [length], page, kv_heads, dim, dtype, garbage=bad)
+    q = _rand(torch, 28, new, heads, dim, dtype=dtype)
+    starts = torch.tensor([0, new], dtype=torch.int32).cuda()
+    lens = torch.tensor([length], dtype=torch.int32).cuda()
+    for window, at, hit in ((0, length - 1, new - 1), (900, length - new - 899, 0)):
+        pools = [c.clone() for c in caches]
+        ref, mag = _attn_ref(_f64(q), held, [new], dim**-0.5, window=window)
+        pools[1][int(tables[0, at // page]), :, at % page] = bad
+        out = cq.cq_attn_paged(q, *pools, tables, lens, length, q_starts=starts, max_q=new, window=window)
+        rest = [i for i in range(new) if i != hit]
+        _within(out[rest], ref[rest], U[dtype] * np.abs(ref[rest]) + (U[dtype] + FP32) * mag[rest] + TINY, "others")
+        assert not bool(torch.isfinite(out[hit]).any())
+
+
 # ---------------------------------------------------------------- streams, graphs, repeats
 
 

@@ -12,17 +12,15 @@ namespace {
 rows_plan plan_rows(int dim, int64_t sequences, int kv_heads, int64_t rows, int64_t tokens, bool keep, bool beside) {
     rows_plan r;
     r.nt = rows <= 16 ? 1 : 2;
-    r.row_tiles = int((rows + 16 * r.nt - 1) / (16 * r.nt));
-    r.numbers = sequences * kv_heads * r.row_tiles;
+    r.numbers = sequences * kv_heads;
     const int64_t units = tokens > 32 ? (tokens + 31) / 32 : 1;
-    r.min_units = 4;  // one tile a wave
     // workgroups that LDS and registers let run at once
     const int64_t most = int64_t(device_cu_count()) * (dim == 256 || beside ? 1 : 2);
     // Up to 1024 tokens one workgroup takes a row tile whole: 800 tokens 12.6 us,
     // 15.3 split and joined (2000 tokens 22.4 and 16.1).  Up to 2048 where the tiles
     // alone fill the chip: 90 sequences of up to 1200 tokens 3 us less.
     r.split = units > (r.numbers >= most ? 64 : 32);
-    const int64_t need = (r.numbers * units + r.min_units - 1) / r.min_units;
+    const int64_t need = (r.numbers * units + kRunUnits - 1) / kRunUnits;
     r.grid = int(r.split ? (need < most ? need : most) : r.numbers);
     r.slots = (r.split ? 2 * int64_t(r.grid) : 0) + (keep ? r.numbers : 0);
     return r;
@@ -93,12 +91,9 @@ join_source place(const pass_plan &t, attn_params &p, uint8_t *ws) {
     join.ml = p.part_ml = reinterpret_cast<float *>(ws + t.o);
     p.keep_parts = t.keep;
     if (t.wide) {
-        join.splits = t.tall.splits;
-        join.rows = t.tall.part_rows ? 1 : 0;
+        join.splits = t.tall.part_rows ? t.tall.splits : 0;
         return join;
     }
-    p.row_tiles = join.row_tiles = t.rows.row_tiles;
-    p.min_units = t.rows.min_units;
     p.shares = t.shares ? reinterpret_cast<int2 *>(ws + t.o + t.ml) : nullptr;
     join.shares = p.shares;
     join.rows = t.shares ? 16 * t.rows.nt : 0;
@@ -219,7 +214,7 @@ hipError_t launch_attn(const cq_kv_cache &c, const cq_attn_args &a, void *worksp
     } else {
         e = launch_pass(dt, c.dim, t.own, p, stream);
     }
-    if (e != hipSuccess || !own.rows) return e;
+    if (e != hipSuccess || (!own.rows && !own.splits)) return e;
     return launch_attn_join(dt, c.dim, p, own, flat, p.tokens * p.heads >= 4096, stream);
 }
 

@@ -56,13 +56,11 @@ struct attn_params {
     float scale, softcap;
     float cap_rate;    // of tanh's argument: scale / softcap, for caps up to kNearCap in powers of two of e^2x
     int flat, flat_len;
-    int row_tiles;     // most row tiles of a sequence
-    int min_units;     // least units of a workgroup (rows kernel)
     int keep_parts;    // every part goes to the workspace
     // rows kernel: [slot][rows of a tile], wide kernel: [split][token][head]
     float *part_o;     // [..][dim], not normalised
     float *part_ml;    // [..][2]: maximum (powers of two), sum
-    int2 *shares;      // [sequence][key head][row tile]: who holds its parts
+    int2 *shares;      // [sequence][key head]: who holds its parts (rows kernel)
 };
 
 // An index array that no kernel writes, at a wave-uniform index: a scalar load.
@@ -339,15 +337,14 @@ __device__ __forceinline__ constexpr int key_place(int row) {  // 16 rows, 16 by
 
 // ---------------------------------------------------------------- launchers
 
-// Rows kernel: a tile of 16 nt rows (queries times the heads of a key head), the
-// tokens shared out over the waves and workgroups.
+// Rows kernel: a sequence's rows (queries times the heads of a key head) are one tile
+// of 16 nt, the tokens shared out over the waves and workgroups.
+constexpr int kRunUnits = 4;  // least 32-token tiles of a workgroup: one a wave
 struct rows_plan {
     int nt;           // 16-row blocks of a tile
     int grid;         // workgroups
-    int row_tiles;    // most row tiles of a sequence
-    int min_units;
     bool split;       // a tile's tokens may be shared out over workgroups
-    int64_t numbers;  // sequences * key heads * row tiles
+    int64_t numbers;  // sequences * key heads
     int64_t slots;    // of the workspace
 };
 hipError_t attn_rows_bf16_64(const rows_plan &r, const attn_params &p, hipStream_t stream);
@@ -385,18 +382,18 @@ hipError_t attn_shared_fp16_128(const wide_plan &w, const attn_params &flat, con
 hipError_t attn_shared_fp16_256(const wide_plan &w, const attn_params &flat, const rows_plan &r, const attn_params &own,
                               hipStream_t stream);
 
-// Where the parts of an output row are: part 0 in the slot `first` + the number of its
-// (sequence, key head, row tile) or `grid` + the workgroup that began it, the next
-// in those of the workgroups that follow; or (splits > 0) at the output row's own
-// place in each split.
+// Where the parts of an output row are.  Of the rows kernel (rows > 0): part 0 in the
+// slot `first` + the number of its (sequence, key head) or `grid` + the workgroup that
+// began it, the next in those of the workgroups that follow.  Of the wide kernel
+// (splits > 0): at the output row's own place in each split.
 struct join_source {
     const float *o, *ml;
     const int2 *shares;
-    int rows;         // of a slot; 0: no such source
-    int row_tiles;
+    int rows;         // of a slot
     int grid, splits;
     int64_t first;    // -1: parts begin at grid + workgroup
 };
+// own: of either kernel; flat: of the wide one, or none.
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
                             bool few, hipStream_t stream);
 

@@ -33,54 +33,36 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
     const int64_t token = row / p.heads;
     const int head = int(row - token * p.heads), kvh = head / p.group, g = head - kvh * p.group;
 
-    // this row's place in each source
-    int64_t number[2] = {0, 0};
-    int at[2] = {0, 0}, first[2] = {0, 0}, count[2] = {0, 0};
+    // this row's place in the slots of the rows kernel
+    int64_t number = 0;
+    int at = 0, first = 0, count = own.splits;
+    int b = int(token), begin = int(token);
+    if (p.q_starts) {
+        int lo = 0, hi = p.batch - 1;  // last b with q_starts[b] <= token
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (p.q_starts[mid] <= token) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+        const seq_t s = sequence(p, b);
+        begin = s.first;
+        if (token < begin || token >= begin + s.n) return;  // a row of no sequence
+    }
     if (own.rows) {
-        int b = int(token), begin = int(token);
-        if (p.q_starts) {
-            int lo = 0, hi = p.batch - 1;  // last b with q_starts[b] <= token
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (p.q_starts[mid] <= token) lo = mid; else hi = mid - 1;
-            }
-            b = lo;
-            const seq_t s = sequence(p, b);
-            begin = s.first;
-            if (token < begin || token >= begin + s.n) return;  // a row of no sequence
-        }
-        count[0] = own.splits;
-        if (!own.splits) {
-            const int r = (int(token) - begin) * p.group + g, rt = r / own.rows;
-            number[0] = (int64_t(b) * p.kv_heads + kvh) * own.row_tiles + rt;
-            at[0] = r - rt * own.rows;
-            const int2 s = own.shares[number[0]];
-            first[0] = s.x;
-            count[0] = s.y;
-        }
+        at = (int(token) - begin) * p.group + g;
+        number = int64_t(b) * p.kv_heads + kvh;
+        const int2 s = own.shares[number];
+        first = s.x;
+        count = s.y;
     }
-    if (flat.rows) {
-        count[1] = flat.splits;
-        if (!flat.splits) {
-            const int64_t r = token * p.group + g, rt = r / flat.rows;
-            number[1] = int64_t(kvh) * flat.row_tiles + rt;
-            at[1] = int(r - rt * flat.rows);
-            const int2 s = flat.shares[number[1]];
-            first[1] = s.x;
-            count[1] = s.y;
-        }
-    }
-    const int parts = count[0] + count[1];
+    const int parts = count + flat.splits;
     if (parts == 0) return;  // written whole
     auto row_at = [&](int k) -> int64_t {
-        const bool f = k >= count[0];
-        const join_source &j = f ? flat : own;
-        const int part = f ? k - count[0] : k;
-        if (j.splits) return part * p.tokens * p.heads + row;
-        return part_slot(j, number[f], first[f], part) * j.rows + at[f];
+        if (own.rows && k < count) return part_slot(own, number, first, k) * own.rows + at;
+        return (k < count ? k : k - count) * p.tokens * p.heads + row;
     };
     auto stat = [&](int k) {
-        return *reinterpret_cast<const float2 *>((k >= count[0] ? flat.ml : own.ml) + row_at(k) * 2);
+        return *reinterpret_cast<const float2 *>((k < count ? own.ml : flat.ml) + row_at(k) * 2);
     };
     // every wave has all maxima; the parts themselves are shared out, kBatch
     // requests of a wave at a time
@@ -100,7 +82,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int kk = min(k0 + k, parts - 1);
-            v[k] = *reinterpret_cast<const fE *>((kk >= count[0] ? flat.o : own.o) + row_at(kk) * D + lane * E);
+            v[k] = *reinterpret_cast<const fE *>((kk < count ? own.o : flat.o) + row_at(kk) * D + lane * E);
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {

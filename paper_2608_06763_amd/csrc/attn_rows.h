@@ -52,20 +52,19 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
 
     int u = 0, u_end = 1, before = 0, b = 0;
     runs_t runs = {1, 1, 0};
-    const int fixed = block;
     if (direct) {
-        b = fixed / (p.kv_heads * p.row_tiles);
+        b = block / p.kv_heads;
     } else {
         const int me = block;
         const place_t at = locate(
-            p.flat ? 1 : p.batch, [&](int b) { return work_of(p, sequence(p, b), R).total; },
+            p.batch, [&](int b) { return work_of(p, sequence(p, b)).total; },
             [&](int all) {
-                const runs_t r = runs_of(p, all, grid);
+                const runs_t r = runs_of(all, grid);
                 return me < r.n ? r.first(me) : -1;
             },
             sched);
         const int total = __builtin_amdgcn_readfirstlane(at.total);
-        runs = runs_of(p, total, grid);
+        runs = runs_of(total, grid);
         if (me >= runs.n || total == 0) return;
         u = runs.first(me);
         u_end = runs.first(me + 1);
@@ -75,13 +74,11 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
 
     while (u < u_end) {
         const seq_t s = sequence_uniform(p, b);
-        const work_t w = work_of(p, s, R);
-        int part, t_begin, t_end;
+        const work_t w = work_of(p, s);
+        int head, t_begin, t_end;
         if (direct) {
-            part = fixed % (p.kv_heads * p.row_tiles);
-            // (key head, row tile) as part_number counts them
-            const int rt = part % p.row_tiles;
-            if (rt >= w.row_tiles) return;
+            if (w.total == 0) return;
+            head = block - b * p.kv_heads;
             t_begin = 0;
             t_end = w.units;
             u = u_end;
@@ -92,16 +89,14 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
                 continue;
             }
             const int in = u - before;
-            part = in / w.units;
-            t_begin = in - part * w.units;
+            head = in / w.units;
+            t_begin = in - head * w.units;
             t_end = min(w.units, t_begin + (u_end - u));
         }
-        const int tiles_of = direct ? p.row_tiles : w.row_tiles;
-        const int head = part / tiles_of, rt = part - head * tiles_of;
-        const int64_t number = part_number(p, b, head, rt);
+        const int64_t number = part_number(p, b, head);
 
         // ---- the rows of this tile
-        const int rows = min(R, s.n * p.group - rt * R);
+        const int rows = s.n * p.group;  // at most R
         const int bidir = p.bidir ? index_at(p.bidir, b) : 0;
         u32x4 q[NT][KS];
         limits_t lim[NT];
@@ -109,8 +104,8 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
         int64_t out_at[NT], q_at[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = rt * R + n * 16 + col;
-            const bool valid = n * 16 + col < rows;
+            const int r = n * 16 + col;
+            const bool valid = r < rows;
             const int i = valid ? r / p.group : 0, hq = head * p.group + (valid ? r - i * p.group : 0);
             lim[n] = limits(p, s, i, valid, bidir);
             slope[n] = p.slopes ? p.slopes[hq] : 0.f;
@@ -128,13 +123,13 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
         }
 
         // ---- the tokens of this part
-        const int32_t *table = p.flat ? p.tables : p.tables + int64_t(b) * p.table_width;
+        const int32_t *table = p.tables + int64_t(b) * p.table_width;
         const int last = (s.len - 1) >> p.page_shift;
         const int held = (s.len + kUnit - 1) / kUnit;  // 0 tiles of an empty sequence
         const int t1 = min(w.tile0 + t_end, held);
         const int first_pos = s.len - s.n, last_pos = s.len - 1;
         // tokens below this are seen by no row
-        const int lo_all = p.window && !p.bidir && !p.flat ? max(0, first_pos - p.window + 1) : 0;
+        const int lo_all = p.window && !p.bidir ? max(0, first_pos - p.window + 1) : 0;
         auto request = [&](const uint16_t *pool, uint32_t dst, const int64_t (&at)[2], auto place) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -217,8 +212,8 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
             }
             vmem_order();
             // ---- softmax
-            bool whole = p.flat ? a + kUnit <= s.len : a + kUnit <= first_pos + 1;
-            if (!p.flat && p.window) whole = whole && a > last_pos - p.window;
+            bool whole = a + kUnit <= first_pos + 1;
+            if (p.window) whole = whole && a > last_pos - p.window;
             uint32_t wt[NT][4], wt2[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -284,7 +279,7 @@ __device__ __forceinline__ void attn_rows_group(const attn_params &p, int block,
                 }
                 return val;
             };
-            if (!whole && !p.flat && (s.n > 1 || p.bidir)) {
+            if (!whole && (s.n > 1 || p.bidir)) {
                 bool odd = false;
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)

@@ -1,6 +1,6 @@
 // How the rows kernel shares its work out, and how its parts are found again.
 //
-// A unit is one 32-token tile of the cache for one key head and one row tile.
+// A unit is one 32-token tile of the cache for one key head, whose rows are one tile.
 // All units of a launch, sequence after sequence, are cut into equal runs, one for
 // each workgroup, so that sequences of any lengths keep every compute unit busy
 // to the end.  The lengths are on the device: every workgroup sums them itself.
@@ -13,19 +13,17 @@ namespace cq {
 constexpr int kUnit = 32;  // tokens
 
 struct work_t {
-    int units;      // of one (key head, row tile)
-    int row_tiles;
-    int tile0;      // first tile that any query sees
-    int total;      // units * row_tiles * kv_heads; the host keeps the sum in 31 bits
+    int units;  // of one key head
+    int tile0;  // first tile that any query sees
+    int total;  // units * kv_heads, or 0 without queries; the host keeps the sum in 31 bits
 };
 
-__device__ __forceinline__ work_t work_of(const attn_params &p, const seq_t &s, int rows) {
+__device__ __forceinline__ work_t work_of(const attn_params &p, const seq_t &s) {
     work_t w;
-    w.row_tiles = (s.n * p.group + rows - 1) / rows;
     w.tile0 = 0;
-    if (p.window && !p.bidir && !p.flat) w.tile0 = max(0, s.len - s.n - p.window + 1) / kUnit;
+    if (p.window && !p.bidir) w.tile0 = max(0, s.len - s.n - p.window + 1) / kUnit;
     w.units = max(1, (s.len + kUnit - 1) / kUnit - w.tile0);
-    w.total = w.units * w.row_tiles * p.kv_heads;
+    w.total = s.n > 0 ? w.units * p.kv_heads : 0;
     return w;
 }
 
@@ -74,7 +72,7 @@ __device__ __forceinline__ place_t locate(int n, Count count, Find find, int *ld
     return {total, lds[5], lds[4]};
 }
 
-// `total` units in equal runs over at most `grid` workgroups of min_units each: the
+// `total` units in equal runs over at most `grid` workgroups of kRunUnits each: the
 // first `more` of the n take one more than `each`.
 struct runs_t {
     int n, each, more;
@@ -84,9 +82,9 @@ struct runs_t {
         return u < big ? u / (each + 1) : more + (u - big) / each;
     }
 };
-__device__ __forceinline__ runs_t runs_of(const attn_params &p, int total, int grid) {
+__device__ __forceinline__ runs_t runs_of(int total, int grid) {
     runs_t r;
-    r.n = max(1, min(grid, (total + p.min_units - 1) / p.min_units));
+    r.n = max(1, min(grid, (total + kRunUnits - 1) / kRunUnits));
     r.each = total / r.n;
     r.more = total - r.each * r.n;
     return r;
@@ -94,10 +92,9 @@ __device__ __forceinline__ runs_t runs_of(const attn_params &p, int total, int g
 
 // Slots of the workspace: workgroup w keeps a part that another workgroup began
 // at slot w, one that it began and another goes on with at slot grid + w; where
-// every part is kept, the first of a (sequence, key head, row tile) at 2 grid +
-// its number.
-__device__ __forceinline__ int64_t part_number(const attn_params &p, int b, int head, int row_tile) {
-    return (int64_t(b) * p.kv_heads + head) * p.row_tiles + row_tile;
+// every part is kept, the first of a (sequence, key head) at 2 grid + its number.
+__device__ __forceinline__ int64_t part_number(const attn_params &p, int b, int head) {
+    return int64_t(b) * p.kv_heads + head;
 }
 
 }  // namespace cq

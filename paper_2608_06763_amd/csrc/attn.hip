@@ -138,10 +138,10 @@ plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
     const int64_t rows = a.tokens * group;
     const bool wide = a.max_q * group > kRowsMost;
     // The prefix always takes the wide kernel, which with few rows is bound by memory
-    // too; where the own tokens take the rows kernel both go in one launch (while its
-    // workgroups are counted in 31 bits): 2 to 8 sequences behind 1500 tokens took
-    // 24-28 us with two launches of the rows kernel, 16 so.
-    t.together = t.shared && !wide && int64_t(a.batch) * c.kv_heads < (int64_t(1) << 29);
+    // too; where the own tokens take the rows kernel both go in one launch: 2 to 8
+    // sequences behind 1500 tokens took 24-28 us with two launches of the rows kernel,
+    // 16 so.
+    t.together = t.shared && !wide;
     t.own = plan_pass(wide, c.dim, a.batch, c.kv_heads, a.max_q * group, rows, t.max_kv, t.shared, t.together);
     t.flat_bytes = 0;
     if (t.shared) {

@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
     constexpr int kBatch = W == 1 ? 2 : 8;  // requests of a wave at a time
     __shared__ float share[3][D + 4];
     const int id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % W;
-    const int64_t row = int64_t(blockIdx.x) * (4 / W) + id / W;
+    const int64_t row = long_index() * (4 / W) + id / W;
     const int lane = threadIdx.x & 63;
     if (row >= p.tokens * p.heads) return;
     const int64_t token = row / p.heads;
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
                             bool few, hipStream_t stream) {
     const int64_t rows = p.tokens * p.heads;
-    const dim3 grid(uint32_t(few ? (rows + 3) / 4 : rows)), block(256);
+    const dim3 grid = long_grid(few ? (rows + 3) / 4 : rows), block(256);
     auto go = [&](auto one, auto four) { hipLaunchKernelGGL(few ? one : four, grid, block, 0, stream, p, own, flat); };
     if (dt == 0) {
         if (dim == 64) go(attn_join_kernel<0, 64, 1>, attn_join_kernel<0, 64, 4>);

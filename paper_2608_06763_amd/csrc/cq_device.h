@@ -134,6 +134,15 @@ __device__ __forceinline__ int exact_carrier(int i, int m, double a, double b) {
     return int(r);
 }
 
+// A launch's threads along x are counted in 32 bits, and what passes them is lost
+// without an error: workgroups past kGridX go along y.
+constexpr int64_t kGridX = int64_t(1) << 21;
+inline dim3 long_grid(int64_t groups) {
+    return groups <= kGridX ? dim3(uint32_t(groups)) : dim3(uint32_t(kGridX), uint32_t((groups + kGridX - 1) / kGridX));
+}
+// of the workgroup; past the last one in the last row of y
+__device__ __forceinline__ int64_t long_index() { return blockIdx.y * kGridX + blockIdx.x; }
+
 // Compute units of the current device, cached per device id.  Host threads
 // may race to fill an entry; they store the same value through an atomic, so
 // the cache is free of data races.

@@ -87,8 +87,8 @@ template <int DT, int RDT, int T, int NV, bool A8>
 __global__ void __launch_bounds__(T == kWave ? 256 : T) norm_residual_kernel(cq_norm_args a, int8_t *x8, float *dx) {
     __shared__ float red[3][T / kWave + 1];
     const int tid = T == kWave ? (threadIdx.x & 63) : threadIdx.x;
-    const int64_t row = T == kWave ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : int64_t(blockIdx.x);
-    if (T == kWave && row >= a.rows) return;  // no barrier in the one-wave form
+    const int64_t row = T == kWave ? long_index() * 4 + (threadIdx.x >> 6) : long_index();
+    if (row >= a.rows) return;  // all of a workgroup, or a wave where none waits for another
     const int width = int(a.width), vecs = width >> 3;
     const int64_t at = row * width;
     const float inv = 1.0f / float(width);
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(T == kWave ? 256 : T) norm_residual_kernel(cq_
 
 template <int DT, int RDT, int T, int NV>
 hipError_t launch_nv(const cq_norm_args &a, int8_t *x8, float *dx, hipStream_t stream) {
-    const dim3 grid(uint32_t(T == kWave ? (a.rows + 3) / 4 : a.rows)), block(T == kWave ? 256 : T);
+    const dim3 grid = long_grid(T == kWave ? (a.rows + 3) / 4 : a.rows), block(T == kWave ? 256 : T);
     if (x8) hipLaunchKernelGGL((norm_residual_kernel<DT, RDT, T, NV, true>), grid, block, 0, stream, a, x8, dx);
     else hipLaunchKernelGGL((norm_residual_kernel<DT, RDT, T, NV, false>), grid, block, 0, stream, a, x8, dx);
     return hipGetLastError();

@@ -38,7 +38,8 @@ __device__ __forceinline__ void words(const float *p, float *v) {
 // One workgroup for a token.
 template <int DT>
 __global__ void __launch_bounds__(512) rope_append_kernel(cq_kv_cache c, cq_rope_args a) {
-    const int64_t token = blockIdx.x;
+    const int64_t token = long_index();
+    if (token >= a.tokens) return;
     const int dim = c.dim, per = dim >> 4, shift = __builtin_ctz(per);  // dim is a power of two
     const int items = (a.heads + 2 * c.kv_heads) << shift;
     const int64_t slot = a.slots[token];
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(512) rope_append_kernel(cq_kv_cache c, cq_rope
 
 hipError_t launch_rope_append(const cq_kv_cache &c, const cq_rope_args &a, hipStream_t stream) {
     const int64_t items = (int64_t(a.heads) + 2 * c.kv_heads) * (c.dim / 16);
-    const dim3 grid(uint32_t(a.tokens)), block(uint32_t(items >= 512 ? 512 : (items + 63) / 64 * 64));
+    const dim3 grid = long_grid(a.tokens), block(uint32_t(items >= 512 ? 512 : (items + 63) / 64 * 64));
     if (c.dtype == CQ_BF16) hipLaunchKernelGGL(rope_append_kernel<0>, grid, block, 0, stream, c, a);
     else hipLaunchKernelGGL(rope_append_kernel<1>, grid, block, 0, stream, c, a);
     return hipGetLastError();

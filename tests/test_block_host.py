@@ -131,6 +131,17 @@ def test_attn_counts_its_work_in_31_bits():
     assert L.cq_attn_workspace_bytes(ref(c), ref(a)) > 0
 
 
+def test_attn_counts_its_workgroups_in_32_bits_of_threads():
+    L = cq.lib()
+    c = cache(kv_heads=8)
+    for batch, want in ((1 << 21, 2), ((1 << 21) + 5, 2), (1 << 20, 0)):
+        a = attn(heads=8, tokens=batch, batch=batch, q_starts=None, max_q=1, max_kv=20, table_width=2)
+        need = L.cq_attn_workspace_bytes(ref(c), ref(a))
+        assert need >= 0 if want == 0 else need == -1
+        if want:
+            assert L.cq_attn_paged(ref(c), ref(a), OK, 1 << 50, None) == want
+
+
 def test_paged_call_takes_no_prefix():
     L = cq.lib()
     assert L.cq_attn_paged(ref(cache()), ref(attn(prefix_table=OK, prefix_len=4)), OK, 1 << 40, None) == 1

@@ -831,3 +831,57 @@ def test_attn_weights_of_few_bf16_rows_keep_two_parts(torch_dev, dim, heads, kv_
     out = cq.cq_attn_paged(q, *caches, tables, torch.tensor(lens, dtype=torch.int32).cuda(), max(lens))
     ref, mag = _attn_ref(_f64(q), held, [1] * len(lens), dim**-0.5)
     _within(out, ref, U["bf16"] * np.abs(ref) + FP32 * mag, "two parts")
+
+
+# ---------------------------------------------------------------- more workgroups than 32 bits of threads
+
+
+def test_norm_of_more_rows_than_a_grid_has_along_x(torch_dev):
+    torch, cq = torch_dev, _cq()
+    rows = (1 << 26) + 5
+    say("norm", rows)
+    pattern = _rand(torch, 91, 1 << 13, 8, dtype="bf16")
+    r = pattern.repeat((rows >> 13) + 1, 1)[:rows]
+    w = _rand(torch, 92, 8, dtype="bf16")
+    want, _ = cq.cq_norm_residual(pattern, w, 1e-5)
+    h, _ = cq.cq_norm_residual(r, w, 1e-5, out=torch.zeros_like(r))
+    assert torch.equal(h[:rows - 5].view(-1, 1 << 13, 8), want.expand(rows >> 13, -1, -1))
+    assert torch.equal(h[-5:], want[:5])
+
+
+def test_append_of_more_tokens_than_a_grid_has_along_x(torch_dev):
+    torch, cq = torch_dev, _cq()
+    tokens = (1 << 26) + 3
+    say("append", tokens)
+    q = torch.empty((tokens, 1, 64), dtype=torch.bfloat16, device="cuda")
+    q.view(-1, 64).copy_(torch.arange(tokens, device="cuda", dtype=torch.int32).remainder(251)[:, None] + 1)
+    slots = torch.full((tokens,), -1, dtype=torch.int32, device="cuda")
+    slots[-1] = 7
+    caches = [torch.zeros((1, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    out = cq.cq_rope_append(q, q, q, None, None, None, slots, *caches, q_out=torch.zeros_like(q))
+    assert torch.equal(out, q)
+    for c in caches:
+        assert torch.equal(c[0, 0, 7], q[-1, 0]) and int(c.count_nonzero()) == 64
+    del q, out, slots
+    torch.cuda.empty_cache()
+
+
+def test_attn_joins_more_rows_than_a_grid_has_along_x(torch_dev):
+    # 2^20 sequences of one query behind one prefix, 64 heads: 2^26 rows, which repeat
+    torch, cq = torch_dev, _cq()
+    batch, heads, dim, repeat = (1 << 20) + 4, 64, 64, 1 << 10
+    say("join", batch, heads)
+    caches, tables, held = _paged(torch, 93, [40], 16, 1, dim, "bf16")
+    few = _rand(torch, 94, repeat, heads, dim, dtype="bf16")
+    q = few.repeat(batch // repeat + 1, 1, 1)[:batch]
+    none = torch.empty((batch, 0), dtype=torch.int32, device="cuda")
+    lens = torch.zeros((batch,), dtype=torch.int32, device="cuda")
+    out = cq.cq_attn_shared_prefix(q, *caches, tables[0].contiguous(), 40, none, lens, 0, out=torch.zeros_like(q))
+    ref, mag = _attn_ref(_f64(few), [[np.zeros((0, 1, dim))] * 2] * repeat, [1] * repeat, dim**-0.5, prefix=held[0])
+    u = U["bf16"]
+    _within(out[:repeat], ref, u * np.abs(ref) + (u + FP32) * mag + TINY, "first rows")
+    for i in range(repeat, batch, repeat):
+        n = min(repeat, batch - i)
+        assert torch.equal(out[i:i + n], out[:n]), i
+    del q, out, none, lens
+    torch.cuda.empty_cache()

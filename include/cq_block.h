@@ -114,8 +114,10 @@ cq_status cq_rope_append(const cq_kv_cache *cache, const cq_rope_args *args, voi
  * see do not reach its output, whatever their keys and values hold.
  *
  * Scores and sums are FP32.  The weights, relative to the largest so far, are
- * rounded to the cache's dtype for the matrix cores (BF16 with up to 32 rows, queries
- * times heads of a key head: carried in two parts).
+ * rounded to the cache's dtype for the matrix cores, and divided by their sum as
+ * rounded; BF16 weights of a sequence's own tokens are carried in two parts where
+ * it has up to 32 rows (max_q times the heads of a key head).  A softcap far above
+ * the scores leaves them as they are.
  */
 typedef struct {
     const void *q;           /* device [tokens, heads, dim] in the cache's dtype,

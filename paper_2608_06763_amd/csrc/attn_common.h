@@ -395,6 +395,6 @@ struct join_source {
 };
 // own: of either kernel; flat: of the wide one, or none.
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
-                            bool few, hipStream_t stream);
+                            bool many, hipStream_t stream);
 
 }  // namespace cq

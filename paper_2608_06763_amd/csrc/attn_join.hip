@@ -1,11 +1,12 @@
 // Joins the parts of an attention output that several workgroups hold: with the
 // largest of their maxima M, o = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k.
-// One workgroup for each query and head, the parts in an order of their own, so
-// that the result does not depend on which workgroup was done first.
+// One workgroup for each query and head, or one wave where there are many, the parts
+// in an order of their own, so that the result does not depend on which workgroup
+// was done first.
 //
 // Bound by latency: a row's places, its statistics, its parts, each after the other,
-// 4 us; the parts are asked for eight at a time (64 parts of 32 rows: 9 us, 30 where
-// one wave asked for one after the other).
+// 4 to 5 us; the parts are asked for eight at a time (64 parts of 32 rows: 7 us, 30
+// where one wave asked for one after the other).
 #include "a8_quant.h"
 #include "attn_common.h"
 
@@ -116,12 +117,12 @@ __global__ void __launch_bounds__(256) attn_join_kernel(attn_params p, join_sour
 
 }  // namespace
 
-// One wave a row where a row has few parts or the rows fill the chip; else four.
+// One wave a row where the rows fill the chip; else four.
 hipError_t launch_attn_join(int dt, int dim, const attn_params &p, const join_source &own, const join_source &flat,
-                            bool few, hipStream_t stream) {
+                            bool many, hipStream_t stream) {
     const int64_t rows = p.tokens * p.heads;
-    const dim3 grid = long_grid(few ? (rows + 3) / 4 : rows), block(256);
-    auto go = [&](auto one, auto four) { hipLaunchKernelGGL(few ? one : four, grid, block, 0, stream, p, own, flat); };
+    const dim3 grid = long_grid(many ? (rows + 3) / 4 : rows), block(256);
+    auto go = [&](auto one, auto four) { hipLaunchKernelGGL(many ? one : four, grid, block, 0, stream, p, own, flat); };
     if (dt == 0) {
         if (dim == 64) go(attn_join_kernel<0, 64, 1>, attn_join_kernel<0, 64, 4>);
         else if (dim == 128) go(attn_join_kernel<0, 128, 1>, attn_join_kernel<0, 128, 4>);

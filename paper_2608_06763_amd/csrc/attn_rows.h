@@ -10,9 +10,9 @@
 // workgroups each keep a maximum, a sum and an output of their own, and join them at
 // the end.
 //
-// Measured: 200001 tokens of 8 key heads of 128 in 138 us, 5.9 TB/s (a plain read of
-// the card: 6.26), and 9 us for the join of 64 parts; 45 sequences of 1000 to 8000
-// tokens in 112 us, 5.4 TB/s, and 6 us; 301 tokens in 8.5 us, which is one workgroup's
+// Measured: 200001 tokens of 8 key heads of 128 in 143 us, 5.7 TB/s (a plain read of
+// the card: 6.26), and 7 us for the join of 64 parts; 45 sequences of 1000 to 8000
+// tokens in 111 us, 5.4 TB/s, and 5 us; 301 tokens in 9.3 us, which is one workgroup's
 // chain of loads: lengths, pages, tokens.
 #pragma once
 

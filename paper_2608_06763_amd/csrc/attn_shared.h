@@ -6,8 +6,8 @@
 // other, a chip's worth at a time, so that a compute unit has one of each.
 //
 // Measured: 90 sequences of up to 1200 tokens behind 24000 shared ones, 32 heads of 128
-// over 8: 74 us where the two took 57 and 47 one after the other, and 11 us for the
-// join; 9 sequences behind 1500: 12 us and 5.
+// over 8: 75 us where the two took 57 and 47 one after the other, and 9 us for the
+// join; 9 sequences behind 1500: 11 us and 5.
 #pragma once
 
 #include "attn_rows.h"

@@ -9,12 +9,18 @@
 // requests are out while the one before is used, and one barrier a tile is enough.
 // Inside a wave the products of the next tile's scores are issued between the
 // exponentials of this one; two workgroups on a compute unit fill each other's waits.
-// Q, the scores of two tiles and O take 192 of the 256 registers that this leaves.
+// Q, the scores of two tiles and O take 160 of the 256 registers that this leaves
+// (heads of 128).
 //
-// Measured: a prompt of 8192 tokens, 32 heads of 128 over 8, BF16: 540 us on a cool
-// card, 1020 TFLOP/s, and 600 us in a row of them (a large matrix product: 1370
-// TFLOP/s); the clock falls from 1.9 to 1.6 GHz meanwhile, so that power bounds it,
-// with the matrix cores busy half of the cycles.  A lone workgroup takes 1.1 us a tile.
+// Weights are rounded to the cache's type in one part, since a second one would take
+// half as many products again: outputs are off from 64 bits by 1.7e-3 of their norm in
+// BF16 and 2.2e-4 in FP16, of which their own rounding is 1.6e-3 and 2.1e-4.
+//
+// Measured: a prompt of 8192 tokens, 32 heads of 128 over 8, BF16: 535 us, 1030
+// TFLOP/s, and 605 us in a row of them (a large matrix product: 1370 TFLOP/s), in which
+// the clock falls from 1.9 to 1.6 GHz.  Of the 1.07e6 cycles a SIMD has products in
+// 5.3e5 and vector work in 4.7e5: in spite of the order of issue the two mostly take
+// turns.  A lone workgroup takes 1.1 us a tile.
 #pragma once
 
 #include "attn_tile.h"
@@ -220,7 +226,7 @@ __device__ __forceinline__ void attn_wide_group(const attn_params &p, int block,
     }
     // One tile: its weights and its second product, beside the first product of the
     // next tile: a product takes the matrix core eight times as long as its issue,
-    // and the exponentials are formed meanwhile.
+    // which leaves room for exponentials of its own wave or of another.
     auto step = [&](auto parity, auto last) {
         constexpr int P = decltype(parity)::value;
         constexpr bool kLast = decltype(last)::value;

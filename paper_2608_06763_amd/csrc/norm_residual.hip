@@ -8,8 +8,10 @@
 // the reductions, 8 elements in a 16-byte vector at a time, so nothing is read
 // twice; the rounded r' is never read back.
 //
-// Measured: 7013 rows of 8192 with post norm and gate 110 us, 5.2 TB/s (a large copy:
-// 4.9); one row of 4096 2.7 us, launch and latency.
+// Measured: 7013 rows of 8192 with post norm and gate 109 us, 5.2 TB/s (a large copy:
+// 4.9), with an FP32 stream 150 us, 5.4 TB/s, to the carriers 112 us, 4.6 TB/s (143 with
+// the quantizer in a call of its own); one row of 4096 2.6 us, launch and latency, to
+// the carriers 3.8 (5.0 in two calls).
 #include "a8_quant.h"
 #include "block_internal.h"
 #include "cq_device.h"

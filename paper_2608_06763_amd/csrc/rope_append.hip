@@ -8,7 +8,7 @@
 // the D / 16 threads of a head write one contiguous run of a page.
 //
 // Measured: 8191 tokens of 64 heads and 8 key heads of 128 in 61 us, 5.5 TB/s (a large
-// copy: 4.9); one token of 32 and 8 heads 2.7 us, launch and latency.
+// copy: 4.9); one token of 32 and 8 heads 2.8 us, launch and latency.
 #include "block_internal.h"
 #include "cq_device.h"
 

@@ -107,12 +107,11 @@ def _on(stream, call, *args):
     block that is let go to the next tensor of the stream that it was made on, and
     one of any other stream would not wait for the kernels.  The stream that was
     current may use what is returned as its own, so letting that go waits for it."""
-    current = torch.cuda.current_stream()
     with torch.cuda.stream(stream):
         got = call(*args)
     for t in got if isinstance(got, tuple) else (got,):
         if not any(t is a for a in args):
-            t.record_stream(current)
+            t.record_stream(torch.cuda.current_stream(t.device))
     return got
 
 

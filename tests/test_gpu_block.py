@@ -690,6 +690,28 @@ def test_block_in_a_graph(torch_dev):
             assert torch.equal(a, b)
 
 
+def test_calls_on_a_side_stream_in_a_graph(torch_dev):
+    torch, cq = torch_dev, _cq()
+    inputs = _block(torch, 43)
+    _run_block(cq, inputs)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        outs = _run_block(cq, inputs, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for seed in (54, 55, 56):
+        fresh = _block(torch, seed)
+        for i in (4, 7):
+            inputs[i].copy_(fresh[i])
+        want = [t.clone() for t in _run_block(cq, inputs)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
 def test_attn_workspace_of_the_caller(torch_dev):
     torch, cq = torch_dev, _cq()
     caches, tables, held = _paged(torch, 61, [3000, 10], 16, 2, 128, "bf16")

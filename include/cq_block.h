@@ -125,9 +125,9 @@ typedef struct {
     void *out;               /* device [tokens, heads, dim], dense               */
     int64_t q_stride;        /* elements, % 8 == 0                               */
     int64_t tokens;          /* rows of q in all; equal to batch without q_starts*/
-    int32_t heads, batch;    /* batch * kv_heads below 2^24, tokens * heads below
-                                2^31 (together: tokens * heads / 128 + (batch +
-                                1) * kv_heads < 2^24)                            */
+    int32_t heads, batch;    /* tokens * heads below 2^31; batch * kv_heads +
+                                tokens * heads / 128 below 2^23 is always taken,
+                                and more while a launch holds its workgroups     */
     const int32_t *q_starts; /* device [batch + 1], ascending from 0 to tokens,
                                 or NULL                                          */
     const int32_t *tables;   /* device [batch, table_width]: the pages of each

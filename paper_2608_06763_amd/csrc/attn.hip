@@ -153,6 +153,16 @@ plan_t make_plan(const cq_kv_cache &c, const cq_attn_args &a) {
 
 }  // namespace
 
+bool attn_fits(const cq_kv_cache &c, const cq_attn_args &a) {
+    const plan_t t = make_plan(c, a);
+    const auto groups = [&](const pass_plan &p) {
+        return p.wide ? p.tall.tiles * c.kv_heads * (t.together ? p.tall.splits : 1) : p.rows.grid;
+    };
+    constexpr int64_t kMost = int64_t(1) << 24;  // of 256 threads, which a launch counts in 32 bits
+    const int64_t own = groups(t.own), flat = t.shared ? groups(t.flat) : 0;
+    return t.together ? own + flat < kMost : own < kMost && flat < kMost;
+}
+
 int64_t attn_workspace_bytes(const cq_kv_cache &c, const cq_attn_args &a) {
     const plan_t t = make_plan(c, a);
     return t.own.bytes() + t.flat_bytes;

@@ -9,7 +9,6 @@
 namespace {
 
 constexpr int64_t kMost = int64_t(1) << 31;
-constexpr int64_t kGroups = int64_t(1) << 24;  // of 256 threads, which a launch counts in 32 bits
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -59,8 +58,6 @@ cq_status check_attn(const cq_kv_cache *c, const cq_attn_args *a, bool shared) {
     // and the units of work (32 tokens of a key head) of all sequences are counted in 31 bits
     const int64_t table = int64_t(a->table_width) * c->page, held = a->max_kv < table ? a->max_kv : table;
     if (int64_t(a->batch) * c->kv_heads >= kMost / (held / 32 + 1)) return CQ_ERR_SHAPE;
-    // the workgroups of a launch: tiles of 128 rows, and one for each sequence and key head
-    if (a->tokens * a->heads / 128 + (int64_t(a->batch) + 1) * c->kv_heads >= kGroups) return CQ_ERR_SHAPE;
     if (!aligned16(a->q) || !aligned16(a->out)) return CQ_ERR_ALIGN;
     if (!aligned4(a->q_starts) || !aligned4(a->tables) || !aligned4(a->kv_lens) || !aligned4(a->slopes) ||
         !aligned4(a->bidir) || !aligned4(a->prefix_table))
@@ -72,7 +69,7 @@ cq_status check_attn(const cq_kv_cache *c, const cq_attn_args *a, bool shared) {
     } else if (a->prefix_table || a->prefix_len) {
         return CQ_ERR_ARG;
     }
-    return CQ_OK;
+    return cq::attn_fits(*c, *a) ? CQ_OK : CQ_ERR_SHAPE;
 }
 
 cq_status attn(const cq_kv_cache *cache, const cq_attn_args *args, bool shared, void *workspace, int64_t bytes,

@@ -134,8 +134,9 @@ def test_attn_counts_its_work_in_31_bits():
 def test_attn_counts_its_workgroups_in_32_bits_of_threads():
     L = cq.lib()
     c = cache(kv_heads=8)
-    for batch, want in ((1 << 21, 2), ((1 << 21) + 5, 2), (1 << 20, 0)):
-        a = attn(heads=8, tokens=batch, batch=batch, q_starts=None, max_q=1, max_kv=20, table_width=2)
+    # one workgroup for each sequence and key head, or few that share the tokens
+    for batch, most, want in ((1 << 21, 20, 2), ((1 << 21) + 5, 20, 2), (1 << 20, 20, 0), ((1 << 21) + 5, 3000, 0)):
+        a = attn(heads=8, tokens=batch, batch=batch, q_starts=None, max_q=1, max_kv=most, table_width=200)
         need = L.cq_attn_workspace_bytes(ref(c), ref(a))
         assert need >= 0 if want == 0 else need == -1
         if want:

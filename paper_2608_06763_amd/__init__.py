@@ -14,7 +14,9 @@ Entry points (same names as the C ABI):
   cq_select_set, cq_select_query, cq_probe_read and cq_probe_wide_rows (measurement aids,
   include/cq_measure.h)
 The operators between the packed products (norms, rotary append, paged
-attention; include/cq_block.h) are bound in ``block.py`` and exported here.
+attention; include/cq_block.h) are bound in ``block.py`` and exported here, and so
+are those of a mixture-of-experts layer (routing, 8-bit products, gated activation,
+sum of the experts; include/cq_experts.h), bound in ``experts.py``.
 The measured kernel-selection tuner that fills the selection table is in
 ``selection.py``.
 """
@@ -38,7 +40,9 @@ EXPORTS = ("cq_status_str", "cq_pack_groups", "cq_decode_ref", "cq_gemm_model_dt
            "cq_family_supported", "cq_gemm_model_dtype_family", "cq_gemm_a8_family", "cq_select_set",
            "cq_select_query", "cq_probe_read", "cq_gemm_routed_model_dtype_noalloc", "cq_set_a8_fused_launch",
            "cq_get_a8_fused_launch", "cq_probe_wide_rows", "cq_norm_residual", "cq_norm_residual_a8",
-           "cq_rope_append", "cq_attn_paged", "cq_attn_shared_prefix", "cq_attn_workspace_bytes")
+           "cq_rope_append", "cq_attn_paged", "cq_attn_shared_prefix", "cq_attn_workspace_bytes", "cq_route",
+           "cq_route_workspace_bytes", "cq_route_plan", "cq_route_plan_workspace_bytes", "cq_gemm_w8",
+           "cq_gemm_routed_w8", "cq_gated", "cq_gated_a8", "cq_combine")
 
 CQ_PATH_MODEL_DTYPE, CQ_PATH_A8 = 0, 1
 FAMILIES = {"auto": 0, "gemv_stream": 1, "gemv_lut": 2, "gemv_narrow": 3, "gemv_generic": 4, "gemm_mfma": 5,
@@ -126,6 +130,7 @@ def lib() -> ctypes.CDLL:
     L.cq_probe_read.restype = ctypes.c_int
     L.cq_probe_read.argtypes = [vp, i64, vp, vp]
     block.declare(L)
+    experts.declare(L)
     _lib = L
     return L
 
@@ -462,4 +467,17 @@ from .block import (  # noqa: E402,F401
     cq_norm_residual,
     cq_norm_residual_a8,
     cq_rope_append,
+)
+
+# ---------------------------------------------------------------- mixture-of-experts layers
+
+from . import experts  # noqa: E402
+from .experts import (  # noqa: E402,F401
+    cq_combine,
+    cq_gated,
+    cq_gated_a8,
+    cq_gemm_routed_w8,
+    cq_gemm_w8,
+    cq_route,
+    cq_route_plan,
 )

@@ -1,4 +1,11 @@
-// Routes in the order of their experts: a stable counting sort.
+// Routes in the order of their experts: a stable counting sort, so that the order is
+// the map's alone.
+//
+// Routes are counted by expert in rows of a table, one row for each run of them.  A
+// workgroup places the routes of a few neighbouring rows: its first place in each expert
+// is what the rows before hold, each of its waves comes behind the waves before, and a
+// wave takes 64 routes at a time, whose lanes of one expert find each other by ballots
+// over the expert's bits.
 #pragma once
 
 #include "cq_device.h"
@@ -6,8 +13,30 @@
 
 namespace cq {
 
-constexpr int kPlanThreads = 256, kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanWaves = 8, kPlanThreads = kPlanWaves * kWave;
 constexpr int kPlanExperts = 1024;  // most
+
+// Rows that a placing workgroup adds up by itself.  Above it a launch of its own turns
+// the table into sums first, since the adding grows with the square of the rows.
+constexpr int kPlanRows = 512;
+
+struct plan_params {
+    int32_t *plan;
+    int32_t *table;   // [rows + 1, experts]: counts; above kPlanRows, what the rows before hold
+    int64_t routes;
+    int row;          // routes of a row
+    int rows, group;  // rows of the table; of a placing workgroup
+    int experts, bits;
+};
+
+inline int plan_bits(int experts) {  // of 0 .. experts
+    int bits = 0;
+    while ((experts >> bits) != 0) ++bits;
+    return bits;
+}
+
+// LDS of a placing workgroup
+inline size_t plan_lds(int experts) { return sizeof(int) * (size_t(kPlanWaves) * (experts + 1) + kPlanThreads); }
 
 // Lanes of the wave that hold the same value as this one (of `bits` bits).
 __device__ __forceinline__ uint64_t same_value(int v, int bits) {
@@ -18,5 +47,148 @@ __device__ __forceinline__ uint64_t same_value(int v, int bits) {
     }
     return same;
 }
+
+__device__ __forceinline__ int plan_bucket(int e, int experts) {
+    return uint32_t(e) < uint32_t(experts) ? e : experts;
+}
+
+// Places of the routes first .. first + count - 1 of the map (count a multiple of the
+// workgroup's threads times STEPS, or all of them); expert_of(i) is the expert of route
+// first + i, or `experts`.  ALONE: there are no other routes, and no table.
+template <bool ALONE, typename F>
+__device__ __forceinline__ void plan_place(const plan_params &p, int block, int64_t first, int count, int *lds, F expert_of) {
+    int *place = lds;  // [wave][expert]: the wave's routes, then the expert's next place
+    int *part = lds + kPlanWaves * (p.experts + 1);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pitch = p.experts + 1;
+    // a wave's routes are neighbours
+    const int share = ((count + kPlanThreads - 1) / kPlanThreads) * kWave, begin = wave * share;
+    const int end = min(begin + share, count);
+    for (int i = tid; i < kPlanWaves * pitch; i += kPlanThreads) place[i] = 0;
+    __syncthreads();
+    for (int i = begin + lane; i < end; i += kWave) atomicAdd(&place[wave * pitch + expert_of(i)], 1);
+    // routes of the rows before this workgroup's, and of all rows, by expert; threads
+    // beyond the experts share the rows out
+    constexpr int kPer = kPlanExperts / kPlanThreads;
+    const int per = (p.experts + kPlanThreads - 1) / kPlanThreads;
+    int before[kPer] = {}, all[kPer] = {};
+    const int row0 = block * p.group;
+    if constexpr (!ALONE) {
+        if (p.rows > kPlanRows) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int e = tid * per + i;
+                if (i >= per || e >= p.experts) continue;
+                before[i] = p.table[int64_t(row0) * p.experts + e];
+                all[i] = p.table[int64_t(p.rows) * p.experts + e];
+            }
+        } else if (per > 1) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int e = tid * per + i;
+                if (i >= per || e >= p.experts) continue;
+#pragma unroll 8
+                for (int b = 0; b < p.rows; ++b) {
+                    const int c = p.table[b * p.experts + e];
+                    all[i] += c;
+                    before[i] += b < row0 ? c : 0;
+                }
+            }
+        } else {
+            // slice s of the rows by the threads s * experts ..: their sums meet in LDS
+            const int slices = kPlanThreads / p.experts, s = tid / p.experts, e = tid - s * p.experts;
+            int some = 0, early = 0;
+            if (s < slices) {
+#pragma unroll 8
+                for (int b = s; b < p.rows; b += slices) {
+                    const int c = p.table[b * p.experts + e];
+                    some += c;
+                    early += b < row0 ? c : 0;
+                }
+            }
+            if (slices > 1) {
+                part[tid] = some;
+                __syncthreads();
+                if (tid < p.experts)
+                    for (int i = 0; i < slices; ++i) all[0] += part[i * p.experts + tid];
+                __syncthreads();
+                part[tid] = early;
+                __syncthreads();
+                if (tid < p.experts)
+                    for (int i = 0; i < slices; ++i) before[0] += part[i * p.experts + tid];
+                __syncthreads();
+            } else if (s == 0) {
+                all[0] = some;
+                before[0] = early;
+            }
+        }
+    }
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int e = tid * per + i;
+        if (i >= per || e >= p.experts) continue;
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int w = 0; w < kPlanWaves; ++w) all[i] += place[w * pitch + e];
+        }
+        sum += all[i];
+    }
+    // offsets of the experts: sums over the lanes of a wave, then over the waves
+    int upto = sum;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int v = __shfl_up(upto, d);
+        if (lane >= d) upto += v;
+    }
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    int at = upto - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+        const int v = part[w];
+        at += w < wave ? v : 0;
+        total += v;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int e = tid * per + i;
+        if (i >= per || e >= p.experts) continue;
+        if (block == 0) p.plan[e] = at;
+        int to = at + before[i];
+#pragma unroll
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int c = place[w * pitch + e];
+            place[w * pitch + e] = to;
+            to += c;
+        }
+        at += all[i];
+    }
+    if (block == 0 && tid == 0) p.plan[p.experts] = total;
+    __syncthreads();
+    int32_t *order = p.plan + p.experts + 1;
+    for (int base = begin; base < end; base += kWave) {
+        const int i = base + lane;
+        const int e = i < end ? expert_of(i) : p.experts;
+        const uint64_t same = same_value(e, p.bits);
+        const int rank = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+        const int to = place[wave * pitch + e] + rank;
+        if (e < p.experts) order[to] = int32_t(first + i);
+        // every lane has read its place before the first of its expert moves it on
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (rank == 0) place[wave * pitch + e] = to + __builtin_popcountll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        // behind the routes that have a place
+        if (i < end && first + i >= total) order[first + i] = -1;
+    }
+}
+
+// Bytes of the table of counts.
+inline int64_t plan_table_bytes(int64_t rows, int experts) { return (rows + 1) * experts * 4; }
+
+// Placing of counted routes; p.group is set here.
+hipError_t launch_plan_place(plan_params p, const int32_t *chosen, hipStream_t stream);
 
 }  // namespace cq

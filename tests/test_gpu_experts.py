@@ -101,9 +101,10 @@ def _route_ref(l, top, scoring="softmax", bias=None, groups=1, kept_groups=1, gr
 
 def _plan_ref(chosen, experts):
     flat = chosen.ravel()
-    at = [np.flatnonzero(flat == e) for e in range(experts)]
-    ends = np.cumsum([0] + [len(a) for a in at])
-    return np.concatenate([ends] + at + [np.full(flat.size - ends[-1], -1)])
+    taken = np.flatnonzero(flat >= 0)
+    order = taken[np.argsort(flat[taken], kind="stable")]
+    ends = np.cumsum(np.concatenate([[0], np.bincount(flat[taken], minlength=experts)]))
+    return np.concatenate([ends, order, np.full(flat.size - taken.size, -1)])
 
 
 def _check_route(torch, logits, top, what, **kw):
@@ -132,7 +133,8 @@ ROUTES = [
 
 @pytest.mark.parametrize("tokens,experts,top", [(1, 1, 1), (1, 8, 2), (3, 7, 7), (1, 128, 8), (5, 60, 4), (70, 64, 6),
                                                 (130, 65, 1), (33, 160, 32), (700, 256, 8), (9, 384, 12), (17, 1000, 10),
-                                                (2, 1024, 32), (1500, 40, 3)])
+                                                (2, 1024, 32), (1500, 40, 3), (64, 512, 15),
+                                                (65, 512, 15), (65, 512, 16), (32, 513, 8), (33, 240, 9), (2000, 128, 2)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_route(torch_dev, tokens, experts, top, dtype):
     torch = torch_dev
@@ -243,7 +245,7 @@ def test_route_of_strided_logits_and_given_outputs(torch_dev):
 
 
 @pytest.mark.parametrize("experts", [1, 2, 64, 100, 1000, 1024])
-@pytest.mark.parametrize("routes", [1, 2, 63, 64, 65, 255, 1000, 1024, 1025, 5000, 70001, 300000])
+@pytest.mark.parametrize("routes", [1, 2, 63, 64, 65, 255, 1000, 1024, 1025, 4096, 4097, 5000, 70001, 300000, 700003])
 def test_route_plan(torch_dev, experts, routes):
     torch, cq = torch_dev, _cq()
     say("plan", experts, routes)

@@ -7,14 +7,14 @@
 // that holds it, and its first slot there; the round's lane later makes the weight.
 //
 // Keys are the logits themselves without a bias (the order of the scores is theirs),
-// else the choices c_e = s_e + b_e in FP32, whose error has a bound.  Where two keys that
-// the result separates lie closer than that (or two sums of a group at the border), the
-// wave takes the token again with keys in FP64: of 8192 tokens over 256 experts about
-// a hundred.  Neighbours of equal logit and bias are a tie, not a doubt.
+// else the choices c_e = s_e + b_e in FP64: of 8192 tokens over 256 experts some always
+// have neighbours closer than FP32 tells apart.  (FP64 multiply-adds issue at the FP32
+// rate.  Keys in FP32 with an error bound, and FP64 for the hundred tokens that it left
+// in doubt, took 29 us for 8191 tokens: one token alone in a wave is 10.)
 //
-// Bound by issue, some 250 instructions a token; the logits are read once.  The tokens
-// of a workgroup are counted by expert on the way, so that one more launch places the
-// routes; up to 64 tokens the one workgroup places them too.
+// Bound by issue; the logits are read once.  The tokens of a workgroup are counted by
+// expert on the way, so that one more launch places the routes; up to 64 tokens the one
+// workgroup places them too.
 #include "experts_internal.h"
 #include "route_plan.h"
 #include "row_vec.h"
@@ -213,19 +213,37 @@ __global__ void __launch_bounds__(256) route_wave_kernel(cq_route_args a) {
 
 // ---------------------------------------------------------------- sixteen lanes a token
 
-// Every lane gets the highest (the sum) of its row of sixteen.
-__device__ __forceinline__ float row_max16(float v) {
-    v = fmaxf(v, dpp_f32<0xb1>(v));
-    v = fmaxf(v, dpp_f32<0x4e>(v));
-    v = fmaxf(v, dpp_f32<0x141>(v));
-    return fmaxf(v, dpp_f32<0x140>(v));
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) { return dpp_f32<CTRL>(v); }
+
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(u)), CTRL, 0xf, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 
-__device__ __forceinline__ float row_sum16(float v) {
-    v += dpp_f32<0xb1>(v);
-    v += dpp_f32<0x4e>(v);
-    v += dpp_f32<0x141>(v);
-    return v + dpp_f32<0x140>(v);
+__device__ __forceinline__ float highest(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double highest(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ float least(float a, float b) { return fminf(a, b); }
+__device__ __forceinline__ double least(double a, double b) { return fmin(a, b); }
+
+// Every lane gets the highest (the sum) of its row of sixteen.
+template <typename K>
+__device__ __forceinline__ K row_max16(K v) {
+    v = highest(v, moved<0xb1>(v));
+    v = highest(v, moved<0x4e>(v));
+    v = highest(v, moved<0x141>(v));
+    return highest(v, moved<0x140>(v));
+}
+
+template <typename K>
+__device__ __forceinline__ K row_sum16(K v) {
+    v += moved<0xb1>(v);
+    v += moved<0x4e>(v);
+    v += moved<0x141>(v);
+    return v + moved<0x140>(v);
 }
 
 struct row_params {
@@ -238,38 +256,72 @@ struct row_params {
     int wide;     // logits of a lane are whole vectors
 };
 
-// The highest two of a and b, each a pair in order.
-__device__ __forceinline__ void merge2(float &hi, float &lo, float hi2, float lo2) {
-    lo = fmaxf(fminf(hi, hi2), fmaxf(lo, lo2));
-    hi = fmaxf(hi, hi2);
+// 1 / v of a finite v >= 1, to 2^-51: the hardware's estimate and two steps of Newton.
+__device__ __forceinline__ double inverse(double v) {
+    double r = __builtin_amdgcn_rcp(v);
+    r = __builtin_fma(__builtin_fma(-v, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-v, r, 1.0), r, r);
 }
 
-template <int CTRL>
-__device__ __forceinline__ void merge_row(float &hi, float &lo) {
-    merge2(hi, lo, dpp_f32<CTRL>(hi), dpp_f32<CTRL>(lo));
+// e^x to 2^-50, without a branch, so that a lane's experts run beside each other: 2^n e^r
+// with |r| <= ln 2 / 2 and e^r by its series up to r^13 (what is left is below 2^-57).
+// Beyond -746 .. 709, where FP64 has no values, the nearest of these.
+__device__ __forceinline__ double exp64(double x) {
+    x = fmin(fmax(x, -746.0), 709.0);
+    const double n = __builtin_rint(x * 1.4426950408889634);
+    // ln 2 in two parts, the first short enough for n times it to be exact
+    const double r = __builtin_fma(n, -1.9082149292705877e-10, __builtin_fma(n, -0.69314718036912382, x));
+    double s = 1.0 / 6227020800.0;
+    s = __builtin_fma(s, r, 1.0 / 479001600.0);
+    s = __builtin_fma(s, r, 1.0 / 39916800.0);
+    s = __builtin_fma(s, r, 1.0 / 3628800.0);
+    s = __builtin_fma(s, r, 1.0 / 362880.0);
+    s = __builtin_fma(s, r, 1.0 / 40320.0);
+    s = __builtin_fma(s, r, 1.0 / 5040.0);
+    s = __builtin_fma(s, r, 1.0 / 720.0);
+    s = __builtin_fma(s, r, 1.0 / 120.0);
+    s = __builtin_fma(s, r, 1.0 / 24.0);
+    s = __builtin_fma(s, r, 1.0 / 6.0);
+    s = __builtin_fma(s, r, 0.5);
+    s = __builtin_fma(s, r, 1.0);
+    s = __builtin_fma(s, r, 1.0);
+    return __builtin_amdgcn_ldexp(s, int(n));
 }
 
-// Of lane (lane + R) % 16 of the row.
-template <int R>
-__device__ __forceinline__ float rotated(float v) { return dpp_f32<0x120 + 16 - R>(v); }
+// Scores in FP64; a softmax's are relative to the highest, which is 1.
+__device__ __forceinline__ double softmax64(float l, float most) {
+    const double e = exp64(double(l) - double(most));
+    return l == most ? 1.0 : e;
+}
+__device__ __forceinline__ double sigmoid64(float l) { return inverse(1.0 + exp64(-double(l))); }
 
+// The highest two of (hi, lo) and of another such pair, by a move inside the row.
+template <int CTRL, typename K>
+__device__ __forceinline__ void merge_row(K &hi, K &lo) {
+    const K hi2 = moved<CTRL>(hi), lo2 = moved<CTRL>(lo);
+    lo = highest(least(hi, hi2), highest(lo, lo2));
+    hi = highest(hi, hi2);
+}
+
+// Logits of experts first .. of a row that starts at `row`; past the last expert any.
 template <int DT, int NE>
-__device__ __forceinline__ void load_run(const row_params &p, int64_t from, int count, float *l) {
+__device__ __forceinline__ void load_run(const row_params &p, int64_t row, int first, float *l) {
     constexpr int V = NE < 8 ? NE : 8;
+    const int last = p.a.experts - 1;
     if (p.wide) {
 #pragma unroll
         for (int c = 0; c < NE; c += V) {
-            if (c >= count) continue;
+            const int64_t from = row + min(first + c, last + 1 - V);
             if constexpr (DT == 2) {
 #pragma unroll
                 for (int h = 0; h < V; h += 4) {
-                    const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.a.logits) + from + c + h);
+                    const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.a.logits) + from + h);
                     l[c + h] = v.x; l[c + h + 1] = v.y; l[c + h + 2] = v.z; l[c + h + 3] = v.w;
                 }
             } else if constexpr (V == 8) {
-                widen8<DT>(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.a.logits) + from + c), l + c);
+                widen8<DT>(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.a.logits) + from), l + c);
             } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.a.logits) + from + c);
+                const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.a.logits) + from);
                 l[c] = act_to_f32<DT>(uint16_t(v.x)); l[c + 1] = act_to_f32<DT>(uint16_t(v.x >> 16));
                 l[c + 2] = act_to_f32<DT>(uint16_t(v.y)); l[c + 3] = act_to_f32<DT>(uint16_t(v.y >> 16));
             }
@@ -277,163 +329,145 @@ __device__ __forceinline__ void load_run(const row_params &p, int64_t from, int 
         return;
     }
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-        if (i < count) l[i] = load_logit<DT>(p.a.logits, from + i);
+    for (int i = 0; i < NE; ++i) l[i] = load_logit<DT>(p.a.logits, row + min(first + i, last));
 }
 
 // One token for each row of sixteen lanes (here: it counts).  `picks`: 16 places of the
-// token.  Returns whether a bound does not separate what the result does; else lane j
-// holds the j-th expert and the weights are written.
+// token.  Lane j gets the j-th expert; the weights are written.
 template <int DT, bool BIASED, int NE>
-__device__ __forceinline__ bool route_row(const row_params &p, int64_t token, bool here, volatile int *picks, int &expert) {
+__device__ __forceinline__ int route_row(const row_params &p, int64_t token, bool here, volatile int *picks) {
+    using K = std::conditional_t<BIASED, double, float>;
     const cq_route_args &a = p.a;
     const int lane = threadIdx.x & 63, l16 = lane & 15;
-    const int gi = l16 & ((1 << p.shift) - 1);
-    const int first = (l16 >> p.shift) * p.size + gi * p.per;
-    const int count = here ? max(0, min(p.per, p.size - gi * p.per)) : 0;
+    const int group = l16 >> p.shift, gi = l16 & ((1 << p.shift) - 1);
+    const int first = group * p.size + gi * p.per;
+    const int count = here && group < p.groups ? max(0, min(p.per, p.size - gi * p.per)) : 0;
     const bool softmax = a.scoring == CQ_SCORE_SOFTMAX;
-    float key[NE];
+    const int64_t row = (token < a.tokens ? token : a.tokens - 1) * a.stride;
+    float l[NE];
+    load_run<DT, NE>(p, row, first, l);
+    float b[BIASED ? NE : 1];
+    if constexpr (BIASED) {
 #pragma unroll
-    for (int i = 0; i < NE; ++i) key[i] = lowest<float>();
-    load_run<DT, NE>(p, token * a.stride + first, count, key);
+        for (int i = 0; i < NE; ++i) b[i] = a.bias[min(first + i, a.experts - 1)];
+    }
     float most = lowest<float>();
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
-        key[i] = i < count ? clean(key[i]) : lowest<float>();
-        most = fmaxf(most, key[i]);
+        l[i] = i < count ? clean(l[i]) : lowest<float>();
+        most = fmaxf(most, l[i]);
     }
-    const bool sums = p.groups > 1 && a.group_top == 2 && !BIASED;  // of scores, beside keys that are logits
+    most = row_max16(most);
+    K key[NE];
     float total = 1.f;
-    bool doubt = false;
-    // Bound of a score's error, absolute.  A difference d of logits with its product by
-    // log2 e is off by 1.2 |d| 2^-23, the exponential by 2^-23 more: (1.2 |d| + 1) e^d
-    // 2^-23 < 2^-22 of the largest e^d, which is 1.  A softmax divides by a sum of up to
-    // 512 such terms: 36 additions of 2^-24 one after the other, and the terms' errors,
-    // weighted, below 2^-19.8: 2^-18 / total with the quotient.  For s = 1 / (1 + e^-l)
-    // the errors of e^-l count s (1 - s) times, and s (1 - s) |l| < 0.23: below 2^-22.
-    float eps = 0x1p-21f;
-    if (softmax && (BIASED || sums || !a.renormalize)) most = row_max16(most);
-    if (softmax && (BIASED || !a.renormalize)) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < NE; ++i)
-            if (key[i] > lowest<float>()) sum += key[i] == most ? 1.f : __expf(key[i] - most);
-        total = row_sum16(sum);
-        eps = 0x1p-18f / total;
-    }
-    auto score = [&](float l) {
-        if (softmax) return (l == most ? 1.f : __expf(l - most));
-        return __builtin_amdgcn_rcpf(1.f + __expf(-l));
-    };
     if constexpr (BIASED) {
-        const float inv = softmax ? __builtin_amdgcn_rcpf(total) : 1.f;
+        double scale = 1.0;
+        if (softmax) {
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
+                key[i] = softmax64(l[i], most);
+                sum += l[i] > lowest<float>() ? key[i] : 0.0;
+            }
+            sum = row_sum16(sum);
+            total = float(sum);
+            scale = inverse(fmax(sum, 1.0));
+        } else {
+#pragma unroll
+            for (int i = 0; i < NE; ++i) key[i] = sigmoid64(l[i]);
+        }
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            if (i < count && key[i] > lowest<float>()) {
-                const float c = __builtin_fmaf(score(key[i]), inv, a.bias[first + i]);
-                key[i] = c == c ? c : lowest<float>();
-            }
+            const double c = __builtin_fma(key[i], scale, double(b[i]));
+            key[i] = l[i] > lowest<float>() && c == c ? c : lowest<double>();
         }
+    } else {
+        if (softmax && !a.renormalize) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < NE; ++i) sum += l[i] > lowest<float>() ? relative_exp<float>(l[i], most) : 0.f;
+            total = row_sum16(sum);
+        }
+#pragma unroll
+        for (int i = 0; i < NE; ++i) key[i] = l[i];
     }
 
     if (p.groups > 1) {
-        float hi = lowest<float>(), lo = lowest<float>();
+        K hi = lowest<K>(), lo = lowest<K>();
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            lo = fmaxf(lo, fminf(hi, key[i]));
-            hi = fmaxf(hi, key[i]);
+            lo = highest(lo, least(hi, key[i]));
+            hi = highest(hi, key[i]);
         }
         if (p.shift > 0) merge_row<0xb1>(hi, lo);
         if (p.shift > 1) merge_row<0x4e>(hi, lo);
         if (p.shift > 2) merge_row<0x141>(hi, lo);
-        // a group's value, and how far it may be off
-        float value = hi, off = 0.f;
-        if (sums) value = hi > lowest<float>() ? score(hi) : lowest<float>();
-        if (BIASED) off = eps + fabsf(hi) * 0x1p-23f;
-        if (a.group_top == 2 && lo > lowest<float>()) {
-            value += sums ? score(lo) : lo;
-            if (BIASED) off += eps + (fabsf(lo) + fabsf(value)) * 0x1p-23f;
+        double value = double(hi);
+        if (a.group_top == 2) {
+            if constexpr (BIASED) {
+                if (lo > lowest<K>()) value += lo;
+            } else if (hi > lowest<K>()) {
+                value = softmax ? softmax64(hi, most) : sigmoid64(hi);
+                if (lo > lowest<K>()) value += softmax ? softmax64(lo, most) : sigmoid64(lo);
+            }
         }
-        // two scores without their common divisor, each at most 1
-        if (sums) off = 0x1p-20f;
-        // lanes of groups that come before this one
+        // lanes of groups that come before this one, by their value or, of equal ones, by
+        // their place: lane (l16 + R) % 16 is behind this one unless it wraps round
         int ahead = 0;
         unroll<1, 16>([&](auto r_c) __attribute__((always_inline)) {
             constexpr int R = decltype(r_c)::value;
-            const float v = rotated<R>(value);
+            const double v = moved<0x120 + 16 - R>(value);
             ahead += v > value || (v == value && l16 >= 16 - R) ? 1 : 0;
         });
-        // those of its own group come first or not by their place in it
-        ahead = (ahead - gi) >> p.shift;
-        const bool kept = ahead < a.kept_groups && value > lowest<float>();
-        if (BIASED || sums) {
-            // the lowest kept group may be no higher than the highest of the others
-            const float least = -row_max16(kept ? off - value : lowest<float>());
-            const float next = row_max16(!kept && value > lowest<float>() ? value + off : lowest<float>());
-            doubt = !(least > next) && next > lowest<float>();
-        }
+        // of its own group's lanes those before it count among them
+        const bool kept = ((ahead - gi) >> p.shift) < a.kept_groups;
 #pragma unroll
-        for (int i = 0; i < NE; ++i) key[i] = kept ? key[i] : lowest<float>();
+        for (int i = 0; i < NE; ++i) key[i] = kept ? key[i] : lowest<K>();
     }
 
     picks[l16] = -1;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    float local = lowest<float>(), mine = lowest<float>();
+    K local = lowest<K>();
 #pragma unroll
-    for (int i = 0; i < NE; ++i) local = fmaxf(local, key[i]);
-    const int rounds = a.top + (BIASED ? 1 : 0);
-    for (int r = 0; r < rounds; ++r) {
-        const float best = row_max16(local);
-        const uint32_t holds = uint32_t(__ballot(local == best && best > lowest<float>()) >> (lane & 48)) & 0xffffu;
+    for (int i = 0; i < NE; ++i) local = highest(local, key[i]);
+    for (int r = 0; r < a.top; ++r) {
+        const K best = row_max16(local);
+        const uint32_t holds = uint32_t(__ballot(local == best && best > lowest<K>()) >> (lane & 48)) & 0xffffu;
         const bool me = (holds & ((2u << l16) - 1u)) == (1u << l16);  // the lowest lane of them
-        if (l16 == r) mine = best;
-        bool found = !me;
-        int slot = 0;
-        local = lowest<float>();
+        int slot = 0;  // the first of its highest
+#pragma unroll
+        for (int i = NE - 1; i >= 0; --i) slot = key[i] == best ? i : slot;
+        const int gone = me ? slot : -1;
+        local = lowest<K>();
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            const bool hit = !found && key[i] == best;
-            found = found || hit;
-            key[i] = hit ? lowest<float>() : key[i];
-            slot = hit ? i : slot;
-            local = fmaxf(local, key[i]);
+            key[i] = i == gone ? lowest<K>() : key[i];
+            local = highest(local, key[i]);
         }
         if (me) picks[r] = first + slot;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int pick = picks[l16];
-    float l = lowest<float>(), b = 0.f;
-    if (pick >= 0) {
-        l = clean(load_logit<DT>(a.logits, token * a.stride + pick));
-        if (BIASED) b = a.bias[pick];
-    }
-    if constexpr (BIASED) {
-        const float next = dpp_f32<0x101>(mine), next_l = dpp_f32<0x101>(l), next_b = dpp_f32<0x101>(b);
-        const bool apart = mine - next > 2.f * eps + (fabsf(mine) + fabsf(next)) * 0x1p-23f;
-        if (l16 < a.top && next > lowest<float>() && !apart && !(l == next_l && b == next_b)) doubt = true;
-    }
-    expert = l16 < a.top ? pick : -1;
-    const uint32_t row = uint32_t(__ballot(doubt && here) >> (lane & 48)) & 0xffffu;
-    if (expert < 0) l = lowest<float>();
-    float w = raw_weight(a, expert, l, row_max16(l), most, total);
+    const int expert = l16 < a.top ? picks[l16] : -1;
+    const float chosen = expert >= 0 ? clean(load_logit<DT>(a.logits, row + expert)) : lowest<float>();
+    float w = raw_weight(a, expert, chosen, row_max16(chosen), most, total);
     if (a.renormalize) {
         const float sum = row_sum16(w);
         if (sum > 0.f) w = w / sum;
     }
-    if (row == 0 && l16 < a.top && token < a.tokens) {
+    if (l16 < a.top && token < a.tokens) {
         a.chosen[token * a.top + l16] = expert;
         a.weights[token * a.top + l16] = expert >= 0 ? w * a.scale : 0.f;
     }
-    return row != 0;
+    return expert;
 }
 
 // PLACE 0: no plan; 1: the workgroup's routes are counted into its row of the table;
 // 2: one workgroup for all tokens, which places them.
 template <int DT, bool BIASED, int NE, int PLACE>
 __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) {
-    extern __shared__ int lds[];
+    extern __shared__ __attribute__((aligned(16))) int lds[];
     __shared__ int picks[kRouteThreads];
-    __shared__ int16_t chosen[PLACE == 0 ? 1 : kBlock * 15 * (PLACE == 2 ? kBlockMost : 1)];
+    __shared__ int16_t chosen[PLACE == 0 ? 1 : kBlock * 16 * (PLACE == 2 ? kBlockMost : 1)];
     const int tid = threadIdx.x, lane = tid & 63, l16 = tid & 15;
     const cq_route_args &a = p.a;
     const int64_t live = a.live ? min(int64_t(max(a.live[0], 0)), a.tokens) : a.tokens;
@@ -445,18 +479,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) 
     const int64_t end = PLACE == 2 ? a.tokens : min((block + 1) * kBlock, a.tokens);
     for (int64_t t0 = block * kBlock; t0 < end; t0 += kBlock) {
         const int64_t token = t0 + (tid >> 4);
-        int expert = -1;
-        const bool again = route_row<DT, BIASED, NE>(p, token, token < live, picks + (tid & ~15), expert);
-        // tokens in doubt, the whole wave for each in turn
-        uint64_t todo = __ballot(again);
-        while (todo) {
-            const int at = __builtin_ctzll(todo) & 48;
-            todo &= ~(uint64_t(0xffff) << at);
-            const int64_t t = t0 + ((tid & ~63) >> 4) + (at >> 4);
-            // the j-th expert is in lane j: to the token's own lanes
-            const int e = __shfl(route_wave<DT, std::conditional_t<BIASED, double, float>, (NE + 3) / 4>(a, t), l16);
-            if ((lane & 48) == at) expert = l16 < a.top ? e : -1;
-        }
+        const int expert = route_row<DT, BIASED, NE>(p, token, token < live, picks + (tid & ~15));
         if constexpr (PLACE != 0) {
             if (l16 < a.top && token < a.tokens) chosen[int(token - block * kBlock) * a.top + l16] = int16_t(expert);
         }
@@ -476,14 +499,14 @@ __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) 
 
 // ---------------------------------------------------------------- host
 
-// Whether sixteen lanes take a token: groups of whole lanes, a lane for each choice and
-// the one behind them, at most 32 experts a lane.
+// Whether sixteen lanes take a token: groups of 1, 2, 4 .. lanes, a lane for each choice,
+// at most 32 experts a lane.
 bool by_rows(const cq_route_args &a, row_params &p) {
     p.a = a;
     p.groups = a.kept_groups < a.groups ? a.groups : 1;
-    if (a.top > 15 || p.groups > 16 || (p.groups & (p.groups - 1))) return false;
-    p.shift = 0;
-    while ((p.groups << p.shift) < 16) ++p.shift;
+    if (a.top > 16 || p.groups > 16) return false;
+    p.shift = 4;
+    while ((p.groups << p.shift) > 16) --p.shift;
     p.size = a.experts / p.groups;
     p.per = (p.size + (1 << p.shift) - 1) >> p.shift;
     if (p.per > 32) return false;
@@ -500,7 +523,7 @@ hipError_t launch_rows(const row_params &p, int place, hipStream_t stream) {
     if (place == 0) hipLaunchKernelGGL((route_row_kernel<DT, BIASED, NE, 0>), grid, block, 0, stream, p);
     else if (place == 1) hipLaunchKernelGGL((route_row_kernel<DT, BIASED, NE, 1>), grid, block,
                                             sizeof(int) * (p.a.experts + 1), stream, p);
-    else hipLaunchKernelGGL((route_row_kernel<DT, BIASED, NE, 2>), grid, block, plan_lds(p.a.experts), stream, p);
+    else hipLaunchKernelGGL((route_row_kernel<DT, BIASED, NE, 2>), grid, block, plan_lds(p.a.experts, true), stream, p);
     return hipGetLastError();
 }
 

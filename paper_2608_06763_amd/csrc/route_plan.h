@@ -35,8 +35,12 @@ inline int plan_bits(int experts) {  // of 0 .. experts
     return bits;
 }
 
-// LDS of a placing workgroup
-inline size_t plan_lds(int experts) { return sizeof(int) * (size_t(kPlanWaves) * (experts + 1) + kPlanThreads); }
+// LDS of a placing workgroup: the waves' places (to whole 16 bytes), sums of threads,
+// and sums of slices of the table, 8 for each thread at most.
+__host__ __device__ inline int plan_pitch(int experts) { return (kPlanWaves * (experts + 1) + 3) & ~3; }
+inline size_t plan_lds(int experts, bool alone) {
+    return sizeof(int) * (size_t(plan_pitch(experts)) + (alone ? 1 : 9) * kPlanThreads);
+}
 
 // Lanes of the wave that hold the same value as this one (of `bits` bits).
 __device__ __forceinline__ uint64_t same_value(int v, int bits) {
@@ -58,7 +62,7 @@ __device__ __forceinline__ int plan_bucket(int e, int experts) {
 template <bool ALONE, typename F>
 __device__ __forceinline__ void plan_place(const plan_params &p, int block, int64_t first, int count, int *lds, F expert_of) {
     int *place = lds;  // [wave][expert]: the wave's routes, then the expert's next place
-    int *part = lds + kPlanWaves * (p.experts + 1);
+    int *part = lds + plan_pitch(p.experts);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pitch = p.experts + 1;
     // a wave's routes are neighbours
     const int share = ((count + kPlanThreads - 1) / kPlanThreads) * kWave, begin = wave * share;
@@ -66,8 +70,7 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
     for (int i = tid; i < kPlanWaves * pitch; i += kPlanThreads) place[i] = 0;
     __syncthreads();
     for (int i = begin + lane; i < end; i += kWave) atomicAdd(&place[wave * pitch + expert_of(i)], 1);
-    // routes of the rows before this workgroup's, and of all rows, by expert; threads
-    // beyond the experts share the rows out
+    // routes of the rows before this workgroup's, and of all rows, by expert
     constexpr int kPer = kPlanExperts / kPlanThreads;
     const int per = (p.experts + kPlanThreads - 1) / kPlanThreads;
     int before[kPer] = {}, all[kPer] = {};
@@ -81,44 +84,52 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
                 before[i] = p.table[int64_t(row0) * p.experts + e];
                 all[i] = p.table[int64_t(p.rows) * p.experts + e];
             }
-        } else if (per > 1) {
+        } else if (p.experts % 4 == 0 && p.experts <= 4 * kPlanThreads / 2) {
+            // four experts a thread, and slices of the rows; their sums meet in LDS
+            const int quads = p.experts / 4, slices = min(kPlanThreads / quads, 16);
+            const int s = tid / quads, e = 4 * (tid - s * quads);
+            int4 some = make_int4(0, 0, 0, 0), early = some;
+            constexpr int kAhead = 16;
+            for (int b0 = s; s < slices && b0 < p.rows; b0 += kAhead * slices) {
+                int4 c[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    c[i] = *reinterpret_cast<const int4 *>(p.table + min(b0 + i * slices, p.rows - 1) * p.experts + e);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int b = b0 + i * slices, in = b < p.rows, first = b < row0;
+                    some.x += in ? c[i].x : 0; some.y += in ? c[i].y : 0;
+                    some.z += in ? c[i].z : 0; some.w += in ? c[i].w : 0;
+                    early.x += first ? c[i].x : 0; early.y += first ? c[i].y : 0;
+                    early.z += first ? c[i].z : 0; early.w += first ? c[i].w : 0;
+                }
+            }
+            int *sums = part + kPlanThreads;  // [2][slices][experts]
+            if (s < slices) {
+                *reinterpret_cast<int4 *>(sums + s * p.experts + e) = some;
+                *reinterpret_cast<int4 *>(sums + (slices + s) * p.experts + e) = early;
+            }
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int e = tid * per + i;
                 if (i >= per || e >= p.experts) continue;
-#pragma unroll 8
+                for (int s = 0; s < slices; ++s) {
+                    all[i] += sums[s * p.experts + e];
+                    before[i] += sums[(slices + s) * p.experts + e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int e = tid * per + i;
+                if (i >= per || e >= p.experts) continue;
+#pragma unroll 16
                 for (int b = 0; b < p.rows; ++b) {
                     const int c = p.table[b * p.experts + e];
                     all[i] += c;
                     before[i] += b < row0 ? c : 0;
                 }
-            }
-        } else {
-            // slice s of the rows by the threads s * experts ..: their sums meet in LDS
-            const int slices = kPlanThreads / p.experts, s = tid / p.experts, e = tid - s * p.experts;
-            int some = 0, early = 0;
-            if (s < slices) {
-#pragma unroll 8
-                for (int b = s; b < p.rows; b += slices) {
-                    const int c = p.table[b * p.experts + e];
-                    some += c;
-                    early += b < row0 ? c : 0;
-                }
-            }
-            if (slices > 1) {
-                part[tid] = some;
-                __syncthreads();
-                if (tid < p.experts)
-                    for (int i = 0; i < slices; ++i) all[0] += part[i * p.experts + tid];
-                __syncthreads();
-                part[tid] = early;
-                __syncthreads();
-                if (tid < p.experts)
-                    for (int i = 0; i < slices; ++i) before[0] += part[i * p.experts + tid];
-                __syncthreads();
-            } else if (s == 0) {
-                all[0] = some;
-                before[0] = early;
             }
         }
     }

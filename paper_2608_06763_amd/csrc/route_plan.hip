@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kWave) plan_sum_kernel(plan_params p) {
 
 template <bool ALONE>
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t *chosen, plan_params p) {
-    extern __shared__ int lds[];
+    extern __shared__ __attribute__((aligned(16))) int lds[];
     const int64_t first = int64_t(blockIdx.x) * p.group * p.row;
     const int count = int(min(int64_t(p.group) * p.row, p.routes - first));
     plan_place<ALONE>(p, blockIdx.x, first, count, lds,
@@ -56,7 +56,7 @@ hipError_t launch_plan_place(plan_params p, const int32_t *chosen, hipStream_t s
     // about a thousand routes a workgroup
     p.group = (kRow + p.row - 1) / p.row;
     hipLaunchKernelGGL((plan_place_kernel<false>), dim3(uint32_t((p.rows + p.group - 1) / p.group)), dim3(kPlanThreads),
-                       plan_lds(p.experts), stream, chosen, p);
+                       plan_lds(p.experts, false), stream, chosen, p);
     return hipGetLastError();
 }
 
@@ -75,7 +75,7 @@ hipError_t launch_route_plan(const int32_t *chosen, int64_t routes, int experts,
     if (routes <= kAlone) {
         p.row = int(routes);
         p.rows = p.group = 1;
-        hipLaunchKernelGGL((plan_place_kernel<true>), dim3(1), dim3(kPlanThreads), plan_lds(experts), stream, chosen, p);
+        hipLaunchKernelGGL((plan_place_kernel<true>), dim3(1), dim3(kPlanThreads), plan_lds(experts, true), stream, chosen, p);
         return hipGetLastError();
     }
     p.row = kRow;

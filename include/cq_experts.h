@@ -98,7 +98,9 @@ typedef struct {
     const float *dw;         /* device [n]; routed: [experts, n]                 */
     const void *bias;        /* device in y_dtype, shaped as dw, or NULL         */
     void *y;                 /* device [rows, n] in y_dtype; routed: [routes, n] */
-    int64_t rows, n, k;      /* k a multiple of 16, at most 131056               */
+    int64_t rows, n, k;      /* k a multiple of 16, at most 131056; fewer than 2^23
+                                tiles of 64 rows (routes; and one for each expert)
+                                by 128 channels                                  */
     int32_t y_dtype;         /* CQ_BF16, CQ_FP16 or CQ_FP32                      */
     int32_t experts;         /* routed only, at most 1024                        */
     const int32_t *plan;     /* routed only: device, of cq_route or cq_route_plan*/

@@ -32,6 +32,18 @@ struct params {
     int y_dt;
 };
 
+// Sum of the lanes up to this one, all lanes active: shifts inside rows of sixteen, then
+// the last lane of a row to the next row, and of the first half to the second.
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast 31 to rows 2 and 3
+    return v;
+}
+
 // Tiles of `tile` routes, one expert each.  Empty: count 0.
 struct place {
     int expert, first, count;  // first: place in the order
@@ -51,12 +63,7 @@ __device__ __forceinline__ place find_tile(const params &p, int t, int tile) {
             n = max(min(p.plan[e + 1], int(p.routes)) - lo, 0);
         }
         const int tiles = (n + tile - 1) / tile;
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
+        const int upto = wave_scan(tiles);
         const int mine = t - before - (upto - tiles);
         const uint64_t found = __ballot(mine >= 0 && mine < tiles);
         if (found) {
@@ -71,6 +78,17 @@ __device__ __forceinline__ place find_tile(const params &p, int t, int tile) {
     return at;
 }
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Resource of weights from channel n0 of an expert on, `channels` rows of k codes; what
+// lies behind them reads zero.  The arguments are made wave-uniform, without which every
+// load would loop over the lanes' resources.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t weights_from(const params &p, int expert, int n0, int channels) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p.w8) + (uint64_t(uniform(expert)) * p.n + uniform(n0)) * p.k;
+    const uint64_t base = uint64_t(uint32_t(uniform(int(at >> 32)))) << 32 | uint32_t(uniform(int(uint32_t(at))));
+    return make_rsrc(reinterpret_cast<const void *>(base), uint32_t(uniform(channels * p.k)));
+}
+
 // Route at place i of the order; one that is none is -1.
 __device__ __forceinline__ int route_at(const params &p, int i) {
     const int r = p.plan[p.experts + 1 + i];
@@ -81,30 +99,59 @@ __device__ __forceinline__ int row_of(const params &p, int route) {
     return p.fan_mul ? int(__umulhi(uint32_t(route), p.fan_mul) >> p.fan_shift) : route;
 }
 
+// Resource of the rows of x that a tile takes: its own of dense ones, all of routed ones
+// (below 2 GiB, checked by the host).
+template <bool ROUTED>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const params &p, const place &at) {
+    uint64_t base = reinterpret_cast<uint64_t>(p.x8);
+    uint32_t bytes = uint32_t(p.rows) * uint32_t(p.k);
+    if constexpr (!ROUTED) {
+        base += uint64_t(uniform(at.first)) * p.k;
+        bytes = uint32_t(uniform(at.count)) * uint32_t(p.k);
+    }
+    base = uint64_t(uint32_t(uniform(int(base >> 32)))) << 32 | uint32_t(uniform(int(uint32_t(base))));
+    return make_rsrc(reinterpret_cast<const void *>(base), uint32_t(uniform(int(bytes))));
+}
+
 template <int YDT>
 __device__ __forceinline__ float load_bias(const void *b, int64_t i) {
     if constexpr (YDT == 2) return static_cast<const float *>(b)[i];
     else return act_to_f32<YDT>(static_cast<const uint16_t *>(b)[i]);
 }
 
-// Four neighbouring outputs at element `to`; whole: all four are there and the place
-// is aligned to them.
+// Four neighbouring values from element i on, at any alignment of an element (the hardware
+// takes wide accesses there; so the copies below become single loads and stores).
+__device__ __forceinline__ float4 load4(const float *p, int64_t i) {
+    float4 v;
+    __builtin_memcpy(&v, p + i, 16);
+    return v;
+}
+
 template <int YDT>
-__device__ __forceinline__ void store4(void *y, int64_t to, const float *v, int count, bool whole) {
-    if (whole) {
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+    if constexpr (YDT == 0) {
+        typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, v2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
+    } else {
+        typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, v2{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+    }
+}
+
+// `count` (at most 4) of four neighbouring outputs at element `to`.
+template <int YDT>
+__device__ __forceinline__ void store4(void *y, int64_t to, const float *v, int count) {
+    if (count == 4) {
         if constexpr (YDT == 2) {
-            *reinterpret_cast<float4 *>(static_cast<float *>(y) + to) = make_float4(v[0], v[1], v[2], v[3]);
+            __builtin_memcpy(static_cast<float *>(y) + to, v, 16);
         } else {
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = YDT == 0 ? f32_to_bf16(v[e]) : f32_to_f16(v[e]);
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(y) + to) =
-                make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+            const uint2 h = make_uint2(pack_out<YDT>(v[0], v[1]), pack_out<YDT>(v[2], v[3]));
+            __builtin_memcpy(static_cast<uint16_t *>(y) + to, &h, 8);
         }
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 3; ++e)
         if (e < count) store_out<YDT>(y, to + e, v[e]);
 }
 
@@ -121,11 +168,16 @@ __device__ __forceinline__ void finish4(const params &p, const i32x4 &sum, float
             v[e] = float(sum[e]) * (dx * p.dw[channel + e]);
             if (p.bias) v[e] += load_bias<YDT>(p.bias, channel + e);
         }
-    store4<YDT>(p.y, row * p.n + n, v, count, (p.n & 3) == 0);
+    store4<YDT>(p.y, row * p.n + n, v, count);
 }
 
-hipError_t launch_rows(const params &p, bool routed, hipStream_t stream);
-hipError_t launch_tile(const params &p, bool routed, hipStream_t stream);
+hipError_t launch_few(const params &p, bool routed, hipStream_t stream);
+hipError_t launch_rows(const params &p, hipStream_t stream);
+// tiles of tile_m rows by tile_n channels: 64 x 128, 64 x 256, 128 x 128, 128 x 256 or
+// 256 x 256; deep: more stages in flight, one workgroup on a compute unit
+hipError_t launch_wide(const params &p, bool routed, int tile_m, int tile_n, bool deep, hipStream_t stream);
+// any size of the rows of x, routed
+hipError_t launch_wide_far(const params &p, hipStream_t stream);
 
 // Tiles of `tile` routes that the plan of `routes` over `experts` can have.
 inline int64_t most_tiles(int64_t routes, int64_t experts, int64_t tile) {

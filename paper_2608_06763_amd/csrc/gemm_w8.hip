@@ -1,6 +1,9 @@
 // Choice of the kernel for an 8-bit product.
 #include "gemm_w8.h"
 
+#include <algorithm>
+#include <cmath>
+
 namespace cq {
 
 namespace {
@@ -31,19 +34,64 @@ w8::params make(const cq_w8_args &a, bool routed) {
     return p;
 }
 
+// Time of a product in tiles, per stage of 128 codes of K and in units of 1 us: rounds over
+// 256 compute units by what a round's stage took on 28672 x 8192, 8192 x 8192 and 4096 x
+// 14336 (64 x 128 tiles wait for memory, 256 x 256 are bound by the matrix cores).
+struct tile_t {
+    int m, n;
+    double cost;
+};
+constexpr tile_t kTiles[] = {{64, 128, 0.46}, {128, 128, 0.60}, {128, 256, 1.05}, {256, 256, 1.78}};
+
+hipError_t dense(const w8::params &p, hipStream_t stream) {
+    auto cells = [&](int m, int n) { return double((p.rows + m - 1) / m) * double((p.n + n - 1) / n); };
+    if (p.rows <= 8) return w8::launch_few(p, false, stream);
+    const tile_t *best = nullptr;
+    double least = 0.0;
+    for (const tile_t &t : kTiles) {
+        const double cost = std::ceil(cells(t.m, t.n) / 256.0) * t.cost;
+        if (!best || cost < least) {
+            best = &t;
+            least = cost;
+        }
+    }
+    // Few rows of few channels: K shared out over a workgroup's waves, whose stage is a step
+    // of each wave's eighth of K (45 rows of 4096 x 14336 19 us, in tiles 50; 48 of 14336 x
+    // 4096 29 and 20).  Up to 16 rows that is the better kernel for all.
+    if (p.rows <= 16 || 0.2 * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::launch_rows(p, stream);
+    return w8::launch_wide(p, false, best->m, best->n, true, stream);
+}
+
+hipError_t routed(const w8::params &p, hipStream_t stream) {
+    if (p.rows * p.k >= int64_t(1) << 31) return w8::launch_wide_far(p, stream);
+    // routes of an expert, were all taken alike
+    const double each = double(p.routes) / p.experts;
+    if (each <= 5.0) return w8::launch_few(p, true, stream);
+    // 128 experts of 2048 x 2048, us: 6 routes each 102 in tiles of 64 x 128 (109 by the few
+    // rows' kernel), 37 each 140 (64 x 256: 140), 62 each 162 (151); 64 experts of 4096 x
+    // 4096: 62 each 292 (267; 128 x 256: 257), 250 each 469 in 128 x 256 (256 x 256: 473),
+    // 500 each 753 (728).
+    const int m = each <= 80.0 ? 64 : each < 400.0 ? 128 : 256, n = each <= 40.0 ? 128 : 256;
+    // a tile of each expert is half full, on average
+    auto cells = [&](int tm, int tn) {
+        return (double(p.routes) / tm + 0.5 * double(std::min<int64_t>(p.experts, p.routes))) * ((p.n + tn - 1) / tn);
+    };
+    if (cells(m, n) >= 256.0) return w8::launch_wide(p, true, m, n, false, stream);
+    const bool low = std::max(1.0, cells(64, 128) / 256.0) * kTiles[0].cost <= std::max(1.0, cells(128, 128) / 256.0) * kTiles[1].cost;
+    return w8::launch_wide(p, true, low ? 64 : 128, 128, true, stream);
+}
+
 }  // namespace
 
 bool w8_fits(const cq_w8_args &a, bool routed) {
-    // workgroups of the smallest tiles, 16 rows by 16 channels
-    const int64_t most = int64_t(1) << 31;
-    const int64_t tiles = routed ? w8::most_tiles(a.routes, a.experts, 16) : (a.rows + 15) / 16;
-    return tiles < most / ((a.n + 15) / 16);
+    // of the smallest of launch_wide's tiles, whose threads along x stay below 2^32
+    const int64_t tiles = routed ? w8::most_tiles(a.routes, a.experts, 64) : (a.rows + 63) / 64;
+    return tiles < (int64_t(1) << 23) / ((a.n + 127) / 128);
 }
 
-hipError_t launch_gemm_w8(const cq_w8_args &a, bool routed, hipStream_t stream) {
-    const w8::params p = make(a, routed);
-    const int64_t rows = routed ? (a.routes + a.experts - 1) / a.experts : a.rows;
-    return rows <= 64 ? w8::launch_rows(p, routed, stream) : w8::launch_tile(p, routed, stream);
+hipError_t launch_gemm_w8(const cq_w8_args &a, bool with_routes, hipStream_t stream) {
+    const w8::params p = make(a, with_routes);
+    return with_routes ? routed(p, stream) : dense(p, stream);
 }
 
 }  // namespace cq

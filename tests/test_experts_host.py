@@ -78,7 +78,7 @@ PRODUCT = [({f: None}, 1) for f in ("x8", "dx", "w8", "dw", "y")] + [
 ] + [({f: BAD}, 3) for f in ("x8", "dx", "w8", "dw", "bias", "y")]
 
 
-@pytest.mark.parametrize("kw,want", PRODUCT + [(dict(rows=1 << 30, n=1 << 20), 2), (dict(plan=OK), 1), (dict(experts=3), 1), (dict(routes=3), 1),
+@pytest.mark.parametrize("kw,want", PRODUCT + [(dict(rows=1 << 30, n=1 << 20), 2), (dict(rows=1 << 29), 2), (dict(plan=OK), 1), (dict(experts=3), 1), (dict(routes=3), 1),
                                                (dict(fan=1), 1)])
 def test_product_refusals(kw, want):
     assert cq.lib().cq_gemm_w8(ref(product(**kw)), None) == want

@@ -2,15 +2,13 @@
 // routes in the order of the experts.
 //
 // Sixteen lanes hold a token's logits, neighbouring experts a lane and whole groups of
-// lanes a group of experts, so that four tokens share every instruction of a wave.  Each
-// round finds the highest key of the sixteen lanes by four row moves, the lowest lane
-// that holds it, and its first slot there; the round's lane later makes the weight.
+// lanes a group of experts, so that four tokens share every instruction of a wave.
 //
 // Keys are the logits themselves without a bias (the order of the scores is theirs),
 // else the choices c_e = s_e + b_e in FP64: of 8192 tokens over 256 experts some always
-// have neighbours closer than FP32 tells apart.  (FP64 multiply-adds issue at the FP32
-// rate.  Keys in FP32 with an error bound, and FP64 for the hundred tokens that it left
-// in doubt, took 29 us for 8191 tokens: one token alone in a wave is 10.)
+// have neighbours closer than FP32 tells apart.  FP64 keys of all experts and a search
+// of all for each choice took 12 us for 8191 tokens, bound by the latency of one wave's
+// instructions; FP32 keys find the few candidates, and FP64 orders those.
 //
 // Bound by issue; the logits are read once.  The tokens of a workgroup are counted by
 // expert on the way, so that one more launch places the routes; up to 64 tokens the one
@@ -332,108 +330,173 @@ __device__ __forceinline__ void load_run(const row_params &p, int64_t row, int f
     for (int i = 0; i < NE; ++i) l[i] = load_logit<DT>(p.a.logits, row + min(first + i, last));
 }
 
-// One token for each row of sixteen lanes (here: it counts).  `picks`: 16 places of the
-// token.  Lane j gets the j-th expert; the weights are written.
+// A place in LDS for each choice of a token (its expert), or for each candidate.
+struct pick_place {
+    int expert;
+    float l, b;
+};
+
+// Logit and bias of one of this lane's experts (its registers have no index: a chain of
+// selections, which is still far from a load's latency).
+template <int NE>
+__device__ __forceinline__ pick_place take(const float (&l)[NE], const float (&b)[NE], int first, int slot) {
+    pick_place o = {first + slot, l[0], b[0]};
+#pragma unroll
+    for (int i = 1; i < NE; ++i) {
+        o.l = slot == i ? l[i] : o.l;
+        o.b = slot == i ? b[i] : o.b;
+    }
+    return o;
+}
+
+// What a row of sixteen lanes knows of its token.
+template <int NE>
+struct row_t {
+    float l[NE], b[NE];  // logits (-infinity: never chosen) and biases of this lane's experts
+    int first;           // the first of them
+    int group_lane;      // this lane's place among its group's
+    float most;          // the highest logit
+    double total;        // of a softmax, relative to `most`
+};
+
 template <int DT, bool BIASED, int NE>
-__device__ __forceinline__ int route_row(const row_params &p, int64_t token, bool here, volatile int *picks) {
-    using K = std::conditional_t<BIASED, double, float>;
+__device__ __forceinline__ row_t<NE> load_row(const row_params &p, int64_t row, bool here) {
     const cq_route_args &a = p.a;
-    const int lane = threadIdx.x & 63, l16 = lane & 15;
-    const int group = l16 >> p.shift, gi = l16 & ((1 << p.shift) - 1);
-    const int first = group * p.size + gi * p.per;
-    const int count = here && group < p.groups ? max(0, min(p.per, p.size - gi * p.per)) : 0;
-    const bool softmax = a.scoring == CQ_SCORE_SOFTMAX;
-    const int64_t row = (token < a.tokens ? token : a.tokens - 1) * a.stride;
-    float l[NE];
-    load_run<DT, NE>(p, row, first, l);
-    float b[BIASED ? NE : 1];
+    const int l16 = threadIdx.x & 15, group = l16 >> p.shift;
+    row_t<NE> t;
+    t.group_lane = l16 & ((1 << p.shift) - 1);
+    t.first = group * p.size + t.group_lane * p.per;
+    const int count = here && group < p.groups ? max(0, min(p.per, p.size - t.group_lane * p.per)) : 0;
+    load_run<DT, NE>(p, row, t.first, t.l);
     if constexpr (BIASED) {
+        if (p.wide) {
 #pragma unroll
-        for (int i = 0; i < NE; ++i) b[i] = a.bias[min(first + i, a.experts - 1)];
-    }
-    float most = lowest<float>();
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-        l[i] = i < count ? clean(l[i]) : lowest<float>();
-        most = fmaxf(most, l[i]);
-    }
-    most = row_max16(most);
-    K key[NE];
-    float total = 1.f;
-    if constexpr (BIASED) {
-        double scale = 1.0;
-        if (softmax) {
-            double sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < NE; ++i) {
-                key[i] = softmax64(l[i], most);
-                sum += l[i] > lowest<float>() ? key[i] : 0.0;
+            for (int i = 0; i < NE; i += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(a.bias + min(t.first + i, a.experts - 4));
+                t.b[i] = v.x; t.b[i + 1] = v.y; t.b[i + 2] = v.z; t.b[i + 3] = v.w;
             }
-            sum = row_sum16(sum);
-            total = float(sum);
-            scale = inverse(fmax(sum, 1.0));
         } else {
 #pragma unroll
-            for (int i = 0; i < NE; ++i) key[i] = sigmoid64(l[i]);
+            for (int i = 0; i < NE; ++i) t.b[i] = a.bias[min(t.first + i, a.experts - 1)];
         }
-#pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            const double c = __builtin_fma(key[i], scale, double(b[i]));
-            key[i] = l[i] > lowest<float>() && c == c ? c : lowest<double>();
-        }
-    } else {
-        if (softmax && !a.renormalize) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < NE; ++i) sum += l[i] > lowest<float>() ? relative_exp<float>(l[i], most) : 0.f;
-            total = row_sum16(sum);
-        }
-#pragma unroll
-        for (int i = 0; i < NE; ++i) key[i] = l[i];
     }
-
-    if (p.groups > 1) {
-        K hi = lowest<K>(), lo = lowest<K>();
+    t.most = lowest<float>();
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            lo = highest(lo, least(hi, key[i]));
-            hi = highest(hi, key[i]);
+    for (int i = 0; i < NE; ++i) {
+        t.l[i] = i < count ? clean(t.l[i]) : lowest<float>();
+        t.most = fmaxf(t.most, t.l[i]);
+    }
+    t.most = row_max16(t.most);
+    t.total = 1.0;
+    if (a.scoring == CQ_SCORE_SOFTMAX && BIASED) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) sum += t.l[i] > lowest<float>() ? softmax64(t.l[i], t.most) : 0.0;
+        t.total = fmax(row_sum16(sum), 1.0);
+    } else if (a.scoring == CQ_SCORE_SOFTMAX && !a.renormalize) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) sum += t.l[i] > lowest<float>() ? relative_exp<float>(t.l[i], t.most) : 0.f;
+        t.total = double(row_sum16(sum));
+    }
+    return t;
+}
+
+// What an expert is chosen by, exactly: its logit, or its score and bias in FP64.
+template <bool BIASED>
+using key_t = std::conditional_t<BIASED, double, float>;
+
+template <bool BIASED>
+__device__ __forceinline__ key_t<BIASED> exact_key(bool softmax, float l, float b, float most, double inv) {
+    if constexpr (BIASED) {
+        const double c = (softmax ? softmax64(l, most) * inv : sigmoid64(l)) + double(b);
+        return l > lowest<float>() && c == c ? c : lowest<double>();
+    } else {
+        return l;
+    }
+}
+
+// Value of this lane's group from the highest two keys of its lanes.
+template <bool BIASED>
+__device__ __forceinline__ double group_value(const cq_route_args &a, key_t<BIASED> hi, key_t<BIASED> lo, float most) {
+    using K = key_t<BIASED>;
+    const bool softmax = a.scoring == CQ_SCORE_SOFTMAX;
+    double value = double(hi);
+    if (a.group_top == 2) {
+        if constexpr (BIASED) {
+            if (lo > lowest<K>()) value += lo;
+        } else if (hi > lowest<K>()) {
+            value = softmax ? softmax64(hi, most) : sigmoid64(hi);
+            if (lo > lowest<K>()) value += softmax ? softmax64(lo, most) : sigmoid64(lo);
         }
-        if (p.shift > 0) merge_row<0xb1>(hi, lo);
-        if (p.shift > 1) merge_row<0x4e>(hi, lo);
-        if (p.shift > 2) merge_row<0x141>(hi, lo);
-        double value = double(hi);
-        if (a.group_top == 2) {
-            if constexpr (BIASED) {
-                if (lo > lowest<K>()) value += lo;
-            } else if (hi > lowest<K>()) {
-                value = softmax ? softmax64(hi, most) : sigmoid64(hi);
-                if (lo > lowest<K>()) value += softmax ? softmax64(lo, most) : sigmoid64(lo);
-            }
-        }
-        // lanes of groups that come before this one, by their value or, of equal ones, by
-        // their place: lane (l16 + R) % 16 is behind this one unless it wraps round
-        int ahead = 0;
-        unroll<1, 16>([&](auto r_c) __attribute__((always_inline)) {
-            constexpr int R = decltype(r_c)::value;
-            const double v = moved<0x120 + 16 - R>(value);
-            ahead += v > value || (v == value && l16 >= 16 - R) ? 1 : 0;
-        });
-        // of its own group's lanes those before it count among them
-        const bool kept = ((ahead - gi) >> p.shift) < a.kept_groups;
+    }
+    return value;
+}
+
+// Whether this lane's group is among the kept: how many lanes' groups come before it, by
+// their value or, of equal ones, by their place (lane (l16 + R) % 16 is behind this one
+// unless it wraps round).
+template <typename V>
+__device__ __forceinline__ bool group_kept(const row_params &p, V value, int group_lane) {
+    const int l16 = threadIdx.x & 15;
+    int ahead = 0;
+    unroll<1, 16>([&](auto r_c) __attribute__((always_inline)) {
+        constexpr int R = decltype(r_c)::value;
+        const V v = moved<0x120 + 16 - R>(value);
+        ahead += v > value || (v == value && l16 >= 16 - R) ? 1 : 0;
+    });
+    // of its own group's lanes those before it count among them
+    return ((ahead - group_lane) >> p.shift) < p.a.kept_groups;
+}
+
+template <typename K, int NE>
+__device__ __forceinline__ void best_two(const row_params &p, const K (&key)[NE], K &hi, K &lo) {
+    hi = lo = lowest<K>();
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+        lo = highest(lo, least(hi, key[i]));
+        hi = highest(hi, key[i]);
+    }
+}
+
+template <typename K>
+__device__ __forceinline__ void merge_group(const row_params &p, K &hi, K &lo) {
+    if (p.shift > 0) merge_row<0xb1>(hi, lo);
+    if (p.shift > 1) merge_row<0x4e>(hi, lo);
+    if (p.shift > 2) merge_row<0x141>(hi, lo);
+}
+
+// The lowest of the lanes of this row for which it holds.
+__device__ __forceinline__ bool first_of_row(bool holds) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    const uint32_t row = uint32_t(__ballot(holds) >> (lane & 48)) & 0xffffu;
+    return (row & ((2u << l16) - 1u)) == (1u << l16);
+}
+
+// The highest keys one after the other, each by a search of all; exact.
+template <bool BIASED, int NE>
+__device__ __forceinline__ void choose_exact(const row_params &p, const row_t<NE> &t, pick_place *picks) {
+    using K = key_t<BIASED>;
+    const cq_route_args &a = p.a;
+    const bool softmax = a.scoring == CQ_SCORE_SOFTMAX;
+    const double inv = BIASED ? inverse(t.total) : 1.0;
+    K key[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) key[i] = exact_key<BIASED>(softmax, t.l[i], t.b[i], t.most, inv);
+    if (p.groups > 1) {
+        K hi, lo;
+        best_two(p, key, hi, lo);
+        merge_group(p, hi, lo);
+        const bool kept = group_kept(p, group_value<BIASED>(a, hi, lo, t.most), t.group_lane);
 #pragma unroll
         for (int i = 0; i < NE; ++i) key[i] = kept ? key[i] : lowest<K>();
     }
-
-    picks[l16] = -1;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     K local = lowest<K>();
 #pragma unroll
     for (int i = 0; i < NE; ++i) local = highest(local, key[i]);
     for (int r = 0; r < a.top; ++r) {
         const K best = row_max16(local);
-        const uint32_t holds = uint32_t(__ballot(local == best && best > lowest<K>()) >> (lane & 48)) & 0xffffu;
-        const bool me = (holds & ((2u << l16) - 1u)) == (1u << l16);  // the lowest lane of them
+        const bool me = first_of_row(local == best && best > lowest<K>());
         int slot = 0;  // the first of its highest
 #pragma unroll
         for (int i = NE - 1; i >= 0; --i) slot = key[i] == best ? i : slot;
@@ -444,12 +507,117 @@ __device__ __forceinline__ int route_row(const row_params &p, int64_t token, boo
             key[i] = i == gone ? lowest<K>() : key[i];
             local = highest(local, key[i]);
         }
-        if (me) picks[r] = first + slot;
+        if (me) picks[r].expert = t.first + slot;
+    }
+}
+
+// The same with a bias, from few candidates: a key that `top` others reach bounds them,
+// found from the highest two of every lane; up to sixteen experts that reach it go to a lane
+// each, where their exact keys are formed and ranked.  Keys up to there are FP32 with a
+// bound on their error.  Returns whether a row needs choose_exact instead: more candidates,
+// or groups at the border closer than the bound tells apart.
+template <int NE>
+__device__ __forceinline__ bool choose_quick(const row_params &p, const row_t<NE> &t, pick_place *picks) {
+    const cq_route_args &a = p.a;
+    const int l16 = threadIdx.x & 15;
+    const bool softmax = a.scoring == CQ_SCORE_SOFTMAX;
+    const double inv = inverse(t.total);
+    // Error of a score: a difference d of logits with its product by log2 e is off by 1.2 |d|
+    // 2^-23, the exponential by 2^-23 more, (1.2 |d| + 1) e^d 2^-23 < 2^-22 of the highest
+    // e^d, which is 1; the divisor is exact.  For s = 1 / (1 + e^-l) the errors of e^-l count
+    // s (1 - s) times, and s (1 - s) |l| < 0.23.  With the roundings below 2^-21 each.
+    const float invf = float(inv), eps = 0x1p-21f * (softmax ? invf : 1.f);
+    float key[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+        const float e = __expf(softmax ? t.l[i] - t.most : -t.l[i]);
+        const float s = softmax ? (t.l[i] == t.most ? 1.f : e) * invf : __builtin_amdgcn_rcpf(1.f + e);
+        const float c = s + t.b[i];
+        key[i] = t.l[i] > lowest<float>() && c == c ? c : lowest<float>();
+    }
+    float hi, lo;
+    best_two(p, key, hi, lo);
+    bool doubt = false;
+    if (p.groups > 1) {
+        float ghi = hi, glo = lo;
+        merge_group(p, ghi, glo);
+        float value = ghi, off = eps + fabsf(ghi) * 0x1p-23f;
+        if (a.group_top == 2 && glo > lowest<float>()) {
+            value += glo;
+            off += eps + (fabsf(glo) + fabsf(value)) * 0x1p-23f;
+        }
+        const bool kept = group_kept(p, value, t.group_lane) && value > lowest<float>();
+        // the lowest kept group has to be above the highest of the others
+        const float floor = -row_max16(kept ? off - value : lowest<float>());
+        const float next = row_max16(!kept && value > lowest<float>() ? value + off : lowest<float>());
+        doubt = next > lowest<float>() && !(floor > next);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) key[i] = kept ? key[i] : lowest<float>();
+        hi = kept ? hi : lowest<float>();
+        lo = kept ? lo : lowest<float>();
+    }
+    float bound = lowest<float>();
+    for (int r = 0; r < a.top; ++r) {
+        bound = row_max16(hi);
+        const bool me = first_of_row(hi == bound && bound > lowest<float>());
+        hi = me ? lo : hi;
+        lo = me ? lowest<float>() : lo;
+    }
+    // what may reach the exact key behind `bound`
+    bound -= 2.f * eps + fminf(fabsf(bound), 3e38f) * 0x1p-22f;
+    uint32_t reach = 0;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) reach |= key[i] >= bound && key[i] > lowest<float>() ? 1u << i : 0u;
+    const int mine = __builtin_popcount(reach);
+    int upto = mine;
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, false);
+    doubt = doubt || upto > 16;
+    if (__any(doubt)) return true;
+    // candidates in the order of their index
+    for (int at = upto - mine; __any(reach != 0); ++at) {
+        if (reach) picks[at] = take(t.l, t.b, t.first, __builtin_ctz(reach));
+        reach &= reach - 1;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int expert = l16 < a.top ? picks[l16] : -1;
+    const pick_place candidate = picks[l16];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    picks[l16].expert = -1;
+    double exact = lowest<double>();
+    if (candidate.expert >= 0) exact = exact_key<true>(softmax, candidate.l, candidate.b, t.most, inv);
+    int rank = 0;
+    unroll<1, 16>([&](auto r_c) __attribute__((always_inline)) {
+        constexpr int R = decltype(r_c)::value;
+        const double v = moved<0x120 + 16 - R>(exact);
+        rank += v > exact || (v == exact && l16 >= 16 - R) ? 1 : 0;
+    });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (candidate.expert >= 0 && rank < a.top) picks[rank].expert = candidate.expert;
+    return false;
+}
+
+// One token for each row of sixteen lanes (here: it counts).  `picks`: 16 places of the
+// token.  Lane j gets the j-th expert; the weights are written.
+template <int DT, bool BIASED, int NE>
+__device__ __forceinline__ int route_row(const row_params &p, int64_t token, bool here, pick_place *picks) {
+    const cq_route_args &a = p.a;
+    const int l16 = threadIdx.x & 15;
+    const int64_t row = (token < a.tokens ? token : a.tokens - 1) * a.stride;
+    const row_t<NE> t = load_row<DT, BIASED, NE>(p, row, here);
+    picks[l16].expert = -1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if constexpr (BIASED) {
+        // with more than twelve to choose, candidates are seldom sixteen at most
+        if (a.top > 12 || choose_quick(p, t, picks)) choose_exact<true, NE>(p, t, picks);
+    } else {
+        choose_exact<false, NE>(p, t, picks);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int expert = l16 < a.top ? picks[l16].expert : -1;
     const float chosen = expert >= 0 ? clean(load_logit<DT>(a.logits, row + expert)) : lowest<float>();
-    float w = raw_weight(a, expert, chosen, row_max16(chosen), most, total);
+    float w = raw_weight(a, expert, chosen, row_max16(chosen), t.most, float(t.total));
     if (a.renormalize) {
         const float sum = row_sum16(w);
         if (sum > 0.f) w = w / sum;
@@ -466,7 +634,7 @@ __device__ __forceinline__ int route_row(const row_params &p, int64_t token, boo
 template <int DT, bool BIASED, int NE, int PLACE>
 __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) {
     extern __shared__ __attribute__((aligned(16))) int lds[];
-    __shared__ int picks[kRouteThreads];
+    __shared__ pick_place picks[kRouteThreads];
     __shared__ int16_t chosen[PLACE == 0 ? 1 : kBlock * 16 * (PLACE == 2 ? kBlockMost : 1)];
     const int tid = threadIdx.x, lane = tid & 63, l16 = tid & 15;
     const cq_route_args &a = p.a;

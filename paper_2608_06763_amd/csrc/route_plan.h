@@ -56,9 +56,8 @@ __device__ __forceinline__ int plan_bucket(int e, int experts) {
     return uint32_t(e) < uint32_t(experts) ? e : experts;
 }
 
-// Places of the routes first .. first + count - 1 of the map (count a multiple of the
-// workgroup's threads times STEPS, or all of them); expert_of(i) is the expert of route
-// first + i, or `experts`.  ALONE: there are no other routes, and no table.
+// Places of the routes first .. first + count - 1 of the map; expert_of(i) is the expert of
+// route first + i, or `experts`.  ALONE: there are no other routes, and no table.
 template <bool ALONE, typename F>
 __device__ __forceinline__ void plan_place(const plan_params &p, int block, int64_t first, int count, int *lds, F expert_of) {
     int *place = lds;  // [wave][expert]: the wave's routes, then the expert's next place
@@ -68,13 +67,19 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
     const int share = ((count + kPlanThreads - 1) / kPlanThreads) * kWave, begin = wave * share;
     const int end = min(begin + share, count);
     for (int i = tid; i < kPlanWaves * pitch; i += kPlanThreads) place[i] = 0;
-    __syncthreads();
-    for (int i = begin + lane; i < end; i += kWave) atomicAdd(&place[wave * pitch + expert_of(i)], 1);
-    // routes of the rows before this workgroup's, and of all rows, by expert
+    // the first routes of a lane stay in registers
+    constexpr int kKeep = 2;
+    int keep[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) keep[i] = begin + i * kWave + lane < end ? expert_of(begin + i * kWave + lane) : p.experts;
+    // Routes of the rows before this workgroup's, and of all rows, by expert: asked for
+    // before the workgroup's own are counted.
     constexpr int kPer = kPlanExperts / kPlanThreads;
     const int per = (p.experts + kPlanThreads - 1) / kPlanThreads;
     int before[kPer] = {}, all[kPer] = {};
     const int row0 = block * p.group;
+    int *sums = part + kPlanThreads;  // of slices of the table: [2][slices][experts]
+    int slices = 0;
     if constexpr (!ALONE) {
         if (p.rows > kPlanRows) {
 #pragma unroll
@@ -84,19 +89,20 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
                 before[i] = p.table[int64_t(row0) * p.experts + e];
                 all[i] = p.table[int64_t(p.rows) * p.experts + e];
             }
-        } else if (p.experts % 4 == 0 && p.experts <= 4 * kPlanThreads / 2) {
-            // four experts a thread, and slices of the rows; their sums meet in LDS
-            const int quads = p.experts / 4, slices = min(kPlanThreads / quads, 16);
+        } else if (p.experts % 4 == 0) {
+            // four experts a thread; the slices' sums meet in LDS
+            const int quads = p.experts / 4;
+            slices = min(kPlanThreads / quads, 16);
             const int s = tid / quads, e = 4 * (tid - s * quads);
             int4 some = make_int4(0, 0, 0, 0), early = some;
-            constexpr int kAhead = 16;
-            for (int b0 = s; s < slices && b0 < p.rows; b0 += kAhead * slices) {
-                int4 c[kAhead];
+            constexpr int kTurn = 32;
+            for (int b0 = s; s < slices && b0 < p.rows; b0 += kTurn * slices) {
+                int4 c[kTurn];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i)
+                for (int i = 0; i < kTurn; ++i)
                     c[i] = *reinterpret_cast<const int4 *>(p.table + min(b0 + i * slices, p.rows - 1) * p.experts + e);
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
+                for (int i = 0; i < kTurn; ++i) {
                     const int b = b0 + i * slices, in = b < p.rows, first = b < row0;
                     some.x += in ? c[i].x : 0; some.y += in ? c[i].y : 0;
                     some.z += in ? c[i].z : 0; some.w += in ? c[i].w : 0;
@@ -104,20 +110,9 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
                     early.z += first ? c[i].z : 0; early.w += first ? c[i].w : 0;
                 }
             }
-            int *sums = part + kPlanThreads;  // [2][slices][experts]
             if (s < slices) {
                 *reinterpret_cast<int4 *>(sums + s * p.experts + e) = some;
                 *reinterpret_cast<int4 *>(sums + (slices + s) * p.experts + e) = early;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int e = tid * per + i;
-                if (i >= per || e >= p.experts) continue;
-                for (int s = 0; s < slices; ++s) {
-                    all[i] += sums[s * p.experts + e];
-                    before[i] += sums[(slices + s) * p.experts + e];
-                }
             }
         } else {
 #pragma unroll
@@ -131,6 +126,18 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
                     before[i] += b < row0 ? c : 0;
                 }
             }
+        }
+    }
+    __syncthreads();
+    auto route = [&](int n) { return n < kKeep ? (n == 0 ? keep[0] : keep[1]) : expert_of(begin + n * kWave + lane); };
+    for (int n = 0; begin + n * kWave + lane < end; ++n) atomicAdd(&place[wave * pitch + route(n)], 1);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int e = tid * per + i;
+        if (i >= per || e >= p.experts) continue;
+        for (int s = 0; s < slices; ++s) {
+            all[i] += sums[s * p.experts + e];
+            before[i] += sums[(slices + s) * p.experts + e];
         }
     }
     __syncthreads();
@@ -178,9 +185,9 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
     if (block == 0 && tid == 0) p.plan[p.experts] = total;
     __syncthreads();
     int32_t *order = p.plan + p.experts + 1;
-    for (int base = begin; base < end; base += kWave) {
-        const int i = base + lane;
-        const int e = i < end ? expert_of(i) : p.experts;
+    for (int n = 0; begin + n * kWave < end; ++n) {
+        const int i = begin + n * kWave + lane;
+        const int e = i < end ? route(n) : p.experts;
         const uint64_t same = same_value(e, p.bits);
         const int rank = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
         const int to = place[wave * pitch + e] + rank;

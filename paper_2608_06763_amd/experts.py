@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import CQError, _stream_ptr, block, lib
+from . import CQError, block, lib
 from .block import _on, _ptr, _type, _types, _vector
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -70,21 +70,26 @@ def declare(L):
 
 
 torch = None  # imported with the first call, as by the package
+_device = _raw_stream = None
 
 
 def _torch():
-    global torch
+    global torch, _device, _raw_stream
     if torch is None:
-        torch = block._torch()
+        t = block._torch()
+        # current device, and handle of its current stream: a tenth of a microsecond each
+        _device, _raw_stream = t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
+        torch = t
     return torch
 
 
-def _here(*tensors):
-    """All lie on the current device: its stream runs the call."""
-    device = torch._C._cuda_getDevice()
+def _begin(*tensors):
+    """The stream of the call, that of the current device, on which all tensors lie."""
+    device = _device()
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError(f"a tensor on {t.device} in a call on cuda:{device}")
+    return _raw_stream(device)
 
 
 def _check(st, where):
@@ -95,7 +100,7 @@ def _check(st, where):
 def _out(t, shape, dtype, like):
     """A given output of this shape and type, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     assert t.dtype == dtype and t.shape == shape and t.is_contiguous()
     return t
 
@@ -105,7 +110,7 @@ def _room(workspace, need, like):
     if workspace is not None:
         assert workspace.is_contiguous()
         return workspace, workspace.numel() * workspace.element_size()
-    return torch.empty((need,), dtype=torch.uint8, device=like.device) if need > 0 else None, need
+    return like.new_empty((need,), dtype=torch.uint8) if need > 0 else None, need
 
 
 # ---------------------------------------------------------------- routing
@@ -124,7 +129,7 @@ def cq_route(logits, top, scoring="softmax", bias=None, groups=1, kept_groups=1,
     if stream is not None:
         return _on(stream, cq_route, logits, top, scoring, bias, groups, kept_groups, group_top, renormalize, scale,
                    live, chosen, weights, plan, workspace)
-    _here(logits, bias, live, chosen, weights, plan, workspace)
+    on = _begin(logits, bias, live, chosen, weights, plan, workspace)
     tokens, experts = logits.shape
     assert logits.stride(1) == 1 or experts == 1
     int32 = torch.int32
@@ -137,7 +142,7 @@ def cq_route(logits, top, scoring="softmax", bias=None, groups=1, kept_groups=1,
                        top, SCORING[scoring], groups, kept_groups, group_top, renormalize, scale)
     L = lib()
     workspace, size = _room(workspace, L.cq_route_workspace_bytes(args) if workspace is None else 0, logits)
-    _check(L.cq_route(args, _ptr(workspace), size, _stream_ptr()), "cq_route")
+    _check(L.cq_route(args, _ptr(workspace), size, on), "cq_route")
     return chosen, weights, plan
 
 
@@ -147,14 +152,14 @@ def cq_route_plan(chosen, experts, plan=None, workspace=None, stream=None):
     _torch()
     if stream is not None:
         return _on(stream, cq_route_plan, chosen, experts, plan, workspace)
-    _here(chosen, plan, workspace)
+    on = _begin(chosen, plan, workspace)
     assert chosen.dtype == torch.int32 and chosen.is_contiguous()
     routes = chosen.numel()
     plan = _out(plan, (experts + 1 + routes,), torch.int32, chosen)
     L = lib()
     workspace, size = _room(workspace, L.cq_route_plan_workspace_bytes(routes, experts) if workspace is None else 0,
                             chosen)
-    _check(L.cq_route_plan(chosen.data_ptr(), routes, experts, plan.data_ptr(), _ptr(workspace), size, _stream_ptr()),
+    _check(L.cq_route_plan(chosen.data_ptr(), routes, experts, plan.data_ptr(), _ptr(workspace), size, on),
            "cq_route_plan")
     return plan
 
@@ -175,7 +180,7 @@ def cq_gemm_w8(x8, dx, w8, dw, bias=None, y_dtype=None, out=None, stream=None):
     _torch()
     if stream is not None:
         return _on(stream, cq_gemm_w8, x8, dx, w8, dw, bias, y_dtype, out)
-    _here(x8, dx, w8, dw, bias, out)
+    on = _begin(x8, dx, w8, dw, bias, out)
     rows, k = x8.shape
     n = w8.shape[0]
     assert w8.shape == (n, k)
@@ -185,7 +190,7 @@ def cq_gemm_w8(x8, dx, w8, dw, bias=None, y_dtype=None, out=None, stream=None):
     args = _W8.pack(_dense8(x8), _vector(dx, rows, torch.float32), _dense8(w8), _vector(dw, n, torch.float32),
                     0 if bias is None else _vector(bias, n, y_dtype), out.data_ptr(), rows, n, k, _type(out), 0, 0, 0,
                     0)
-    _check(lib().cq_gemm_w8(args, _stream_ptr()), "cq_gemm_w8")
+    _check(lib().cq_gemm_w8(args, on), "cq_gemm_w8")
     return out
 
 
@@ -199,7 +204,7 @@ def cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=1, bias=None, y_dtype=None, out=
     _torch()
     if stream is not None:
         return _on(stream, cq_gemm_routed_w8, x8, dx, w8, dw, plan, fan, bias, y_dtype, out)
-    _here(x8, dx, w8, dw, plan, bias, out)
+    on = _begin(x8, dx, w8, dw, plan, bias, out)
     rows, k = x8.shape
     experts, n, _ = w8.shape
     assert w8.shape[2] == k and dw.shape == (experts, n) and dw.dtype == torch.float32 and dw.is_contiguous()
@@ -212,7 +217,7 @@ def cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=1, bias=None, y_dtype=None, out=
     args = _W8.pack(_dense8(x8), _vector(dx, rows, torch.float32), _dense8(w8), dw.data_ptr(), _ptr(bias),
                     out.data_ptr(), rows, n, k, _type(out), experts, _vector(plan, plan.numel(), torch.int32), routes,
                     fan)
-    _check(lib().cq_gemm_routed_w8(args, _stream_ptr()), "cq_gemm_routed_w8")
+    _check(lib().cq_gemm_routed_w8(args, on), "cq_gemm_routed_w8")
     return out
 
 
@@ -234,9 +239,9 @@ def cq_gated(gate, up, act="silu", out=None, stream=None):
     _torch()
     if stream is not None:
         return _on(stream, cq_gated, gate, up, act, out)
-    _here(gate, up, out)
-    out = _out(out, gate.shape, gate.dtype, gate)
-    _check(lib().cq_gated(_gated_args(gate, up, act, out), _stream_ptr()), "cq_gated")
+    on = _begin(gate, up, out)
+    out = gate.new_empty(gate.shape) if out is None else _out(out, gate.shape, gate.dtype, gate)
+    _check(lib().cq_gated(_gated_args(gate, up, act, out), on), "cq_gated")
     return out
 
 
@@ -246,12 +251,12 @@ def cq_gated_a8(gate, up, act="silu", out=None, x8=None, dx=None, stream=None):
     _torch()
     if stream is not None:
         return _on(stream, cq_gated_a8, gate, up, act, out, x8, dx)
-    _here(gate, up, out, x8, dx)
+    on = _begin(gate, up, out, x8, dx)
     if out is not None:
         _out(out, gate.shape, gate.dtype, gate)
     x8 = _out(x8, gate.shape, torch.int8, gate)
     dx = _out(dx, gate.shape[:1], torch.float32, gate)
-    _check(lib().cq_gated_a8(_gated_args(gate, up, act, out), x8.data_ptr(), dx.data_ptr(), _stream_ptr()),
+    _check(lib().cq_gated_a8(_gated_args(gate, up, act, out), x8.data_ptr(), dx.data_ptr(), on),
            "cq_gated_a8")
     return x8, dx
 
@@ -266,7 +271,7 @@ def cq_combine(y, weights, chosen, experts, base=None, alpha=1.0, out=None, stre
     _torch()
     if stream is not None:
         return _on(stream, cq_combine, y, weights, chosen, experts, base, alpha, out)
-    _here(y, weights, chosen, base, out)
+    on = _begin(y, weights, chosen, base, out)
     tokens, top = chosen.shape
     routes, width = y.shape
     assert routes == tokens * top and y.is_contiguous()
@@ -280,5 +285,5 @@ def cq_combine(y, weights, chosen, experts, base=None, alpha=1.0, out=None, stre
     out = _out(out, (tokens, width), dtype, y)
     args = _COMBINE.pack(y.data_ptr(), weights.data_ptr(), chosen.data_ptr(), _ptr(base), out.data_ptr(), tokens, width,
                          top, experts, _type(y), _types[dtype], alpha)
-    _check(lib().cq_combine(args, _stream_ptr()), "cq_combine")
+    _check(lib().cq_combine(args, on), "cq_combine")
     return out

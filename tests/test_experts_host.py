@@ -156,7 +156,7 @@ def test_packed_arguments_are_whole_structures():
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
     torch = E._torch()
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(E, "_device", lambda: 0)
     f, i = torch.zeros((4, 64)), torch.zeros((4, 64), dtype=torch.int8)
     h, c = f.bfloat16(), torch.zeros((4, 2), dtype=torch.int32)
     plan = torch.zeros((13,), dtype=torch.int32)
@@ -192,7 +192,7 @@ def test_calls_given_a_stream_allocate_and_launch_there(monkeypatch):
                 return 0
             return call
 
-    empty = torch.empty
+    empty = torch.Tensor.new_empty
 
     def make(*args, **kw):
         made.append(now[-1])
@@ -204,10 +204,9 @@ def test_calls_given_a_stream_allocate_and_launch_there(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", on)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: now[-1])
     monkeypatch.setattr(E, "lib", Library)
-    monkeypatch.setattr(E, "_here", lambda *t: None)
-    monkeypatch.setattr(E, "_stream_ptr", lambda stream=None: 0)
+    monkeypatch.setattr(E, "_begin", lambda *t: 0)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: used.append((t.data_ptr(), s)))
-    monkeypatch.setattr(torch, "empty", make)
+    monkeypatch.setattr(torch.Tensor, "new_empty", make)
     calls = [(4, lambda s: cq.cq_route(f, 2, stream=s)), (2, lambda s: cq.cq_route_plan(c, 4, stream=s)),
              (1, lambda s: cq.cq_gemm_w8(i, v, i, v, stream=s)),
              (1, lambda s: cq.cq_gemm_routed_w8(i, v, i.view(4, 1, 64), v.view(4, 1), plan, stream=s)),
@@ -225,7 +224,7 @@ def test_calls_given_a_stream_allocate_and_launch_there(monkeypatch):
 
 def test_arguments_of_other_shapes_and_types_are_refused(monkeypatch):
     torch = E._torch()
-    monkeypatch.setattr(E, "_here", lambda *t: None)
+    monkeypatch.setattr(E, "_begin", lambda *t: 0)
     f, i = torch.zeros((4, 64)), torch.zeros((4, 64), dtype=torch.int8)
     h, c, v = f.bfloat16(), torch.zeros((2, 2), dtype=torch.int32), torch.zeros((4,))
     w, plan = torch.zeros((2, 2)), torch.zeros((9,), dtype=torch.int32)

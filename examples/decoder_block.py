@@ -1,10 +1,13 @@
 """A decoder block on packed weights, from prompts to single tokens.
 
 Every step of the block runs in this framework's kernels: norms with the residual
-stream, packed products, rotary positions with the append to a paged cache, and
-attention over the cache (the activation of the gated product is PyTorch's).
+stream, packed products, rotary positions with the append to a paged cache,
+attention over the cache, and the gated activation.  With --experts the gated
+layers are a mixture of experts in 8-bit integers: a router's choice, the experts'
+products on the carriers of the activations, and their sum by the router's weights.
 
     python examples/decoder_block.py            # a small block, checked against FP32
+    python examples/decoder_block.py --experts 16 --top 4
     python examples/decoder_block.py --layers 8 --width 4096 --heads 32 --kv-heads 8 --ffn 14336 --tokens 64
 
 It takes several prompts of different lengths in one call, decodes tokens for all of
@@ -36,16 +39,58 @@ def packed(g, n: int, k: int):
     return cq.CQWeight.from_codes(codes.numpy(), scale.numpy(), one, zero, BITS, GROUP)
 
 
+class Experts:
+    """Gated layers of which every token takes `top`, in 8-bit integers with a scale for
+    each channel, and their router."""
+
+    def __init__(self, g, width, ffn, experts, top):
+        self.ffn, self.experts, self.top = ffn, experts, top
+        self.router = packed(g, experts, width)
+        self.bias = (0.01 * torch.randn(experts, generator=g)).cuda()
+        self.up, self.down = self.weights(g, 2 * ffn, width), self.weights(g, width, ffn)
+        self.errors = []
+
+    def weights(self, g, n, k):
+        w = torch.randn((self.experts, n, k), generator=g).cuda() * k**-0.5
+        scale = w.abs().amax(-1) / 127.0
+        return torch.round(w / scale[..., None]).to(torch.int8), scale
+
+    def __call__(self, h, check):
+        """h [tokens, width], the normed stream; returns the experts' sum."""
+        logits = cq.cq_gemm_model_dtype(self.router, h, y_dtype=torch.float32)
+        chosen, weights, plan = cq.cq_route(logits, self.top, scoring="sigmoid", bias=self.bias)
+        x8, dx = cq.cq_quantize_act_a8(h)
+        pair = cq.cq_gemm_routed_w8(x8, dx, *self.up, plan, fan=self.top)
+        h8, dh = cq.cq_gated_a8(*pair.split(self.ffn, dim=1))
+        y = cq.cq_combine(cq.cq_gemm_routed_w8(h8, dh, *self.down, plan), weights, chosen, self.experts)
+        if check:
+            want = self.plain(h.float(), chosen, weights)
+            self.errors.append(float((y.float() - want).norm() / want.norm()))
+        return y
+
+    def plain(self, x, chosen, weights):
+        """The same in FP32 from the choice on."""
+        out = torch.zeros_like(x)
+        up, down = (w.float() * scale[..., None] for w, scale in (self.up, self.down))
+        for j in range(self.top):
+            for t, e in enumerate(chosen[:, j].tolist()):
+                gate, rest = (up[e] @ x[t]).split(self.ffn)
+                out[t] += weights[t, j] * (down[e] @ (torch.nn.functional.silu(gate) * rest))
+        return out
+
+
 class Block:
     """Weights of one decoder block, its pages of the cache, and its forward pass."""
 
-    def __init__(self, width, heads, kv_heads, dim, ffn, pages, page, seed, a8=False):
+    def __init__(self, width, heads, kv_heads, dim, ffn, pages, page, seed, a8=False, experts=0, top=2):
         g = torch.Generator().manual_seed(seed)
         self.heads, self.kv_heads, self.dim, self.ffn, self.a8 = heads, kv_heads, dim, ffn, a8
         self.qkv = packed(g, (heads + 2 * kv_heads) * dim, width)
         self.o = packed(g, width, heads * dim)
-        self.up = packed(g, 2 * ffn, width)
-        self.down = packed(g, width, ffn)
+        self.experts = Experts(g, width, ffn, experts, top) if experts else None
+        if not experts:
+            self.up = packed(g, 2 * ffn, width)
+            self.down = packed(g, width, ffn)
         self.norms = [(1.0 + 0.1 * torch.randn(width, generator=g)).to(torch.bfloat16).cuda() for _ in range(2)]
         self.k, self.v = (torch.zeros((pages, kv_heads, page, dim), dtype=torch.bfloat16, device="cuda")
                           for _ in range(2))
@@ -72,9 +117,11 @@ class Block:
             a = cq.cq_attn_paged(q, self.k, self.v, step["tables"], step["lens"], step["max_kv"],
                                  q_starts=step["starts"], max_q=step["max_q"])
         a = cq.cq_gemm_model_dtype(self.o, a.view(t, -1))
+        if self.experts:
+            h, stream = cq.cq_norm_residual(stream, self.norms[1], EPS, y=a)
+            return stream, self.experts(h, step["check"])
         gated, stream = self.product(self.up, stream, self.norms[1], a)
-        gate, up = gated.split(self.ffn, dim=1)
-        return stream, cq.cq_gemm_model_dtype(self.down, torch.nn.functional.silu(gate) * up)
+        return stream, cq.cq_gemm_model_dtype(self.down, cq.cq_gated(*gated.split(self.ffn, dim=1)))
 
 
 class Pages:
@@ -156,12 +203,14 @@ def plain_forward(blocks, x, rope, segments):
 
 
 def serve(layers=2, width=1024, heads=8, kv_heads=2, dim=128, ffn=2816, prompts=(37, 5, 130), tokens=4, samples=6,
-          page=16, a8=False, check=True):
+          page=16, a8=False, check=True, experts=0, top=2):
     """Prompts, then `tokens` tokens of each; then the same for `samples` continuations
-    of the last prompt.  Returns the relative errors against FP32 (check), or times."""
+    of the last prompt.  Returns the relative errors against FP32 (check), or times: of
+    each sequence, or of each call of the experts, given their choice, which a sequence's
+    small errors may turn."""
     longest = max(prompts) + tokens + 1
     pages = sum(-(-(n + tokens) // page) for n in prompts) + samples * -(-tokens // page)
-    blocks = [Block(width, heads, kv_heads, dim, ffn, pages, page, seed, a8) for seed in range(layers)]
+    blocks = [Block(width, heads, kv_heads, dim, ffn, pages, page, seed, a8, experts, top) for seed in range(layers)]
     rope, book = rope_tables(longest, dim), Pages(pages, page, -(-longest // page))
     g = torch.Generator().manual_seed(99)
     seq = {s: torch.randn((n + tokens, width), generator=g).to(torch.bfloat16).cuda() for s, n in enumerate(prompts)}
@@ -170,6 +219,7 @@ def serve(layers=2, width=1024, heads=8, kv_heads=2, dim=128, ffn=2816, prompts=
 
     def run(x, new, prefix=None):
         step = book.step(new, prefix)
+        step["check"] = check
         torch.cuda.synchronize()
         begin = time.perf_counter()
         y = forward(blocks, x, rope, step)
@@ -189,6 +239,8 @@ def serve(layers=2, width=1024, heads=8, kv_heads=2, dim=128, ffn=2816, prompts=
         tail.append(run(more[:, i].contiguous(), {("sample", j): 1 for j in range(samples)}, prefix=base))
     if not check:
         return times
+    if experts:
+        return [e for b in blocks for e in b.experts.errors]
     errors = []
 
     def compare(a, b):
@@ -207,14 +259,14 @@ def serve(layers=2, width=1024, heads=8, kv_heads=2, dim=128, ffn=2816, prompts=
 def main():
     p = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("layers", 2), ("width", 1024), ("heads", 8), ("kv-heads", 2), ("ffn", 2816), ("tokens", 4),
-                        ("samples", 6)):
+                        ("samples", 6), ("experts", 0), ("top", 2)):
         p.add_argument(f"--{name}", type=int, default=value)
     p.add_argument("--a8", action="store_true", help="products of the normed stream over Dynamic-A8")
     a = p.parse_args()
     sizes = {k: v for k, v in vars(a).items()}
     if a.width <= 1024:
         errors = serve(**sizes)
-        print("relative error against FP32, each sequence:", " ".join(f"{e:.4f}" for e in errors))
+        print("relative error against FP32, each", "call of the experts:" if a.experts else "sequence:", " ".join(f"{e:.4f}" for e in errors))
     else:
         times = serve(**sizes, prompts=(900, 2000, 1100), check=False)
         n = a.tokens

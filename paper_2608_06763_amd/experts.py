@@ -225,11 +225,13 @@ def cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=1, bias=None, y_dtype=None, out=
 
 
 def _gated_args(gate, up, act, out):
-    rows, width = gate.shape
-    assert up.shape == gate.shape and up.dtype == gate.dtype
-    assert gate.stride(1) == 1 and up.stride(1) == 1 and (rows == 1 or up.stride(0) == gate.stride(0))
+    shape, strides = gate.shape, gate.stride()
+    rows, width = shape
+    assert up.shape == shape and up.dtype == gate.dtype
     # the stride of a single row is never used: any legal one serves
-    return _GATED.pack(gate.data_ptr(), up.data_ptr(), _ptr(out), rows, width, gate.stride(0) if rows > 1 else width,
+    stride = strides[0] if rows > 1 else width
+    assert strides[1] == 1 and (up.stride() == strides or rows == 1 and up.stride(1) == 1)
+    return _GATED.pack(gate.data_ptr(), up.data_ptr(), 0 if out is None else out.data_ptr(), rows, width, stride,
                        _type(gate), ACTIVATIONS[act])
 
 
@@ -240,7 +242,8 @@ def cq_gated(gate, up, act="silu", out=None, stream=None):
     if stream is not None:
         return _on(stream, cq_gated, gate, up, act, out)
     on = _begin(gate, up, out)
-    out = gate.new_empty(gate.shape) if out is None else _out(out, gate.shape, gate.dtype, gate)
+    # an empty_like is dense here, and takes two thirds of a new_empty's time
+    out = torch.empty_like(gate) if out is None else _out(out, gate.shape, gate.dtype, gate)
     _check(lib().cq_gated(_gated_args(gate, up, act, out), on), "cq_gated")
     return out
 
@@ -280,9 +283,10 @@ def cq_combine(y, weights, chosen, experts, base=None, alpha=1.0, out=None, stre
     if base is not None:
         assert base.shape == (tokens, width) and base.is_contiguous()
         dtype = base.dtype
+        out = torch.empty_like(base) if out is None else _out(out, (tokens, width), dtype, y)
     else:
         dtype = y.dtype if out is None else out.dtype
-    out = _out(out, (tokens, width), dtype, y)
+        out = _out(out, (tokens, width), dtype, y)
     args = _COMBINE.pack(y.data_ptr(), weights.data_ptr(), chosen.data_ptr(), _ptr(base), out.data_ptr(), tokens, width,
                          top, experts, _type(y), _types[dtype], alpha)
     _check(lib().cq_combine(args, on), "cq_combine")

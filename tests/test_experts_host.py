@@ -192,11 +192,11 @@ def test_calls_given_a_stream_allocate_and_launch_there(monkeypatch):
                 return 0
             return call
 
-    empty = torch.Tensor.new_empty
-
-    def make(*args, **kw):
-        made.append(now[-1])
-        return empty(*args, **kw)
+    def maker(empty):
+        def make(*args, **kw):
+            made.append(now[-1])
+            return empty(*args, **kw)
+        return make
 
     f, i = torch.zeros((4, 64)), torch.zeros((4, 64), dtype=torch.int8)
     h, c, plan = f.bfloat16(), torch.zeros((2, 2), dtype=torch.int32), torch.zeros((9,), dtype=torch.int32)
@@ -206,7 +206,8 @@ def test_calls_given_a_stream_allocate_and_launch_there(monkeypatch):
     monkeypatch.setattr(E, "lib", Library)
     monkeypatch.setattr(E, "_begin", lambda *t: 0)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: used.append((t.data_ptr(), s)))
-    monkeypatch.setattr(torch.Tensor, "new_empty", make)
+    for where, name in ((torch, "empty_like"), (torch.Tensor, "new_empty")):
+        monkeypatch.setattr(where, name, maker(getattr(where, name)))
     calls = [(4, lambda s: cq.cq_route(f, 2, stream=s)), (2, lambda s: cq.cq_route_plan(c, 4, stream=s)),
              (1, lambda s: cq.cq_gemm_w8(i, v, i, v, stream=s)),
              (1, lambda s: cq.cq_gemm_routed_w8(i, v, i.view(4, 1, 64), v.view(4, 1), plan, stream=s)),

@@ -359,6 +359,58 @@ def test_routed_product(torch_dev, experts, tokens, top, n, k, fan):
         _within(got[torch.from_numpy(at).cuda()], ref[at], _product_bound(ref, mag, b, dtype)[at], "routed")
 
 
+def _check_on_device(torch, got, x8, dx, w8, dw, bias, dtype, what):
+    """The same bound as above, formed on the device in FP64 (its sums are exact too)."""
+    mag = (x8.double() @ w8.double().t()) * dx.double()[:, None] * dw.double()
+    b = torch.zeros_like(mag) if bias is None else bias.double().expand_as(mag)
+    ref = mag + b
+    off = (got.double() - ref).abs() - (U[dtype] * ref.abs() * (1.0 + 4.0 * E) + 4.0 * E * (mag.abs() + b.abs()) + TINY)
+    assert bool((off <= 0).all()), (what, float(off.max()))
+
+
+@pytest.mark.parametrize("rows,n,k", [(9, 28667, 144), (16, 40000, 1040), (31, 28667, 272), (64, 28667, 144), (65, 30000, 128),
+                                      (128, 28667, 656), (129, 20001, 144), (256, 28667, 400), (383, 20008, 16), (1000, 28667, 144),
+                                      (1025, 16385, 528), (2500, 8191, 1168)])
+def test_product_of_many_tiles(torch_dev, rows, n, k):
+    torch, cq = torch_dev, _cq()
+    x8, w8 = _int8(torch, rows + k, rows, k), _int8(torch, n + k, n, k)
+    dx, dw = _scales(torch, 1, rows), _scales(torch, 2, n)
+    for dtype, biased in (("bf16", False), ("fp16", True), ("fp32", True)):
+        say("product of many tiles", rows, n, k, dtype, biased)
+        bias = _rand(torch, 3, n, dtype=dtype) if biased else None
+        room = torch.full((rows * n + 64,), 7.0, dtype=_dtype(torch, dtype), device="cuda")
+        got = cq.cq_gemm_w8(x8, dx, w8, dw, bias=bias, out=room[:rows * n].view(rows, n))
+        _check_on_device(torch, got, x8, dx, w8, dw, bias, dtype, (rows, n, k, dtype))
+        assert bool((room[rows * n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("experts,tokens,top,n,k", [(64, 400, 4, 1001, 272), (64, 900, 4, 1000, 144), (32, 1000, 4, 1703, 400),
+                                                    (16, 3000, 3, 1704, 144), (8, 60, 2, 8000, 512), (128, 60, 8, 700, 1040),
+                                                    (3, 5000, 1, 5000, 48)])
+@pytest.mark.parametrize("fan", [True, False])
+def test_routed_product_of_many_tiles(torch_dev, experts, tokens, top, n, k, fan):
+    torch, cq = torch_dev, _cq()
+    g = torch.Generator().manual_seed(experts * tokens)
+    w8, dw = _int8(torch, 1, experts, n, k), _scales(torch, 2, experts, n)
+    rows = tokens if fan else tokens * top
+    x8, dx = _int8(torch, 3, rows, k), _scales(torch, 4, rows)
+    # some experts far more in demand than others, some routes of none
+    chosen = (torch.rand((tokens, top), generator=g) ** 2 * (experts + 1)).long() - 1
+    flat = chosen.flatten().cuda()
+    plan = cq.cq_route_plan(chosen.to(torch.int32).cuda(), experts)
+    for dtype, biased in (("bf16", True), ("fp32", False)):
+        say("routed product of many tiles", experts, tokens, top, n, k, fan, dtype)
+        bias = _rand(torch, 5, experts, n, dtype=dtype) if biased else None
+        out = torch.full((tokens * top, n), 77.0, dtype=_dtype(torch, dtype), device="cuda")
+        cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=top if fan else 1, bias=bias, out=out)
+        assert bool((out[flat < 0] == 77.0).all())
+        for e in range(experts):
+            r = (flat == e).nonzero()[:, 0]
+            at = r // top if fan else r
+            if r.numel():
+                _check_on_device(torch, out[r], x8[at], dx[at], w8[e], dw[e], None if bias is None else bias[e], dtype, e)
+
+
 def test_routed_product_equals_the_dense_one(torch_dev):
     # every route with the one expert: the same numbers, whatever the tiles
     torch, cq = torch_dev, _cq()
@@ -654,3 +706,11 @@ def test_layer_in_two_graphs(torch_dev, tokens):
             torch.cuda.synchronize()
             for a, b in zip(want, outs):
                 assert torch.equal(a, b)
+
+
+def test_decoder_block_example_with_experts(torch_dev):
+    from examples.decoder_block import serve
+    errors = serve(experts=8, top=3, tokens=2, ffn=512, samples=3)
+    # carriers are off by up to half a step, 1 / 254 of a row's largest value, which for
+    # products of two normal values is up to some fifteen times their root mean square
+    assert len(errors) == 2 * 5 and max(errors) < 15.0 / 254.0 + 2.0**-7

@@ -546,11 +546,36 @@ __device__ __forceinline__ bool choose_quick(const row_params &p, const row_t<NE
             value += glo;
             off += eps + (fabsf(glo) + fabsf(value)) * 0x1p-23f;
         }
-        const bool kept = group_kept(p, value, t.group_lane) && value > lowest<float>();
+        bool kept = group_kept(p, value, t.group_lane) && value > lowest<float>();
         // the lowest kept group has to be above the highest of the others
         const float floor = -row_max16(kept ? off - value : lowest<float>());
         const float next = row_max16(!kept && value > lowest<float>() ? value + off : lowest<float>());
         doubt = next > lowest<float>() && !(floor > next);
+        if (__any(doubt)) {
+            // one token in some ten thousand: the groups again, from exact keys of every
+            // lane's highest two, which they are if the third is out of reach
+            int first = NE, second = NE;
+#pragma unroll
+            for (int i = NE - 1; i >= 0; --i) first = key[i] == hi ? i : first;
+#pragma unroll
+            for (int i = NE - 1; i >= 0; --i) second = key[i] == lo && i != first ? i : second;
+            float third = lowest<float>();
+#pragma unroll
+            for (int i = 0; i < NE; ++i) third = fmaxf(third, i == first || i == second ? lowest<float>() : key[i]);
+            const bool near = third > lowest<float>() && !(lo - third > 2.f * eps + (fabsf(lo) + fabsf(third)) * 0x1p-23f);
+            const pick_place one = take(t.l, t.b, t.first, first), two = take(t.l, t.b, t.first, second);
+            double ehi = lowest<double>(), elo = ehi;
+            if (hi > lowest<float>()) ehi = exact_key<true>(softmax, one.l, one.b, t.most, inv);
+            if (lo > lowest<float>()) elo = exact_key<true>(softmax, two.l, two.b, t.most, inv);
+            const double top = highest(ehi, elo);
+            elo = least(ehi, elo);
+            ehi = top;
+            merge_group(p, ehi, elo);
+            const bool exactly = group_kept(p, group_value<true>(a, ehi, elo, t.most), t.group_lane);
+            const int lane = threadIdx.x & 63;
+            kept = doubt ? exactly : kept;
+            doubt = doubt && (uint32_t(__ballot(near) >> (lane & 48)) & 0xffffu) != 0;
+        }
 #pragma unroll
         for (int i = 0; i < NE; ++i) key[i] = kept ? key[i] : lowest<float>();
         hi = kept ? hi : lowest<float>();

@@ -67,11 +67,11 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
     const int share = ((count + kPlanThreads - 1) / kPlanThreads) * kWave, begin = wave * share;
     const int end = min(begin + share, count);
     for (int i = tid; i < kPlanWaves * pitch; i += kPlanThreads) place[i] = 0;
-    // the first routes of a lane stay in registers
-    constexpr int kKeep = 2;
+    // the first routes of a lane stay in registers, asked for together
+    constexpr int kKeep = 8;
     int keep[kKeep];
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) keep[i] = begin + i * kWave + lane < end ? expert_of(begin + i * kWave + lane) : p.experts;
+    for (int n = 0; n < kKeep; ++n) keep[n] = begin + n * kWave + lane < end ? expert_of(begin + n * kWave + lane) : p.experts;
     // Routes of the rows before this workgroup's, and of all rows, by expert: asked for
     // before the workgroup's own are counted.
     constexpr int kPer = kPlanExperts / kPlanThreads;
@@ -129,8 +129,10 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
         }
     }
     __syncthreads();
-    auto route = [&](int n) { return n < kKeep ? (n == 0 ? keep[0] : keep[1]) : expert_of(begin + n * kWave + lane); };
-    for (int n = 0; begin + n * kWave + lane < end; ++n) atomicAdd(&place[wave * pitch + route(n)], 1);
+#pragma unroll
+    for (int n = 0; n < kKeep; ++n)
+        if (begin + n * kWave + lane < end) atomicAdd(&place[wave * pitch + keep[n]], 1);
+    for (int i = begin + kKeep * kWave + lane; i < end; i += kWave) atomicAdd(&place[wave * pitch + expert_of(i)], 1);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = tid * per + i;
@@ -185,9 +187,7 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
     if (block == 0 && tid == 0) p.plan[p.experts] = total;
     __syncthreads();
     int32_t *order = p.plan + p.experts + 1;
-    for (int n = 0; begin + n * kWave < end; ++n) {
-        const int i = begin + n * kWave + lane;
-        const int e = i < end ? route(n) : p.experts;
+    auto put = [&](int i, int e) __attribute__((always_inline)) {
         const uint64_t same = same_value(e, p.bits);
         const int rank = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
         const int to = place[wave * pitch + e] + rank;
@@ -200,7 +200,12 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
         __builtin_amdgcn_wave_barrier();
         // behind the routes that have a place
         if (i < end && first + i >= total) order[first + i] = -1;
-    }
+    };
+#pragma unroll
+    for (int n = 0; n < kKeep; ++n)
+        if (begin + n * kWave < end) put(begin + n * kWave + lane, keep[n]);
+    for (int base = begin + kKeep * kWave; base < end; base += kWave)
+        put(base + lane, base + lane < end ? expert_of(base + lane) : p.experts);
 }
 
 // Bytes of the table of counts.

@@ -366,7 +366,6 @@ __device__ __forceinline__ row_t<NE> load_row(const row_params &p, int64_t row, 
     row_t<NE> t;
     t.group_lane = l16 & ((1 << p.shift) - 1);
     t.first = group * p.size + t.group_lane * p.per;
-    const int count = here && group < p.groups ? max(0, min(p.per, p.size - t.group_lane * p.per)) : 0;
     load_run<DT, NE>(p, row, t.first, t.l);
     if constexpr (BIASED) {
         if (p.wide) {
@@ -380,6 +379,9 @@ __device__ __forceinline__ row_t<NE> load_row(const row_params &p, int64_t row, 
             for (int i = 0; i < NE; ++i) t.b[i] = a.bias[min(t.first + i, a.experts - 1)];
         }
     }
+    // behind the loads, since whether the token counts is itself a load
+    __builtin_amdgcn_sched_barrier(0);
+    const int count = here && group < p.groups ? max(0, min(p.per, p.size - t.group_lane * p.per)) : 0;
     t.most = lowest<float>();
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
@@ -663,7 +665,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) 
     __shared__ int16_t chosen[PLACE == 0 ? 1 : kBlock * 16 * (PLACE == 2 ? kBlockMost : 1)];
     const int tid = threadIdx.x, lane = tid & 63, l16 = tid & 15;
     const cq_route_args &a = p.a;
-    const int64_t live = a.live ? min(int64_t(max(a.live[0], 0)), a.tokens) : a.tokens;
+    const int32_t *counts = a.live;
+    const int live = counts ? *counts : 0x7fffffff;  // tokens are fewer
     if constexpr (PLACE == 1) {
         for (int e = tid; e <= a.experts; e += kRouteThreads) lds[e] = 0;
     }
@@ -672,7 +675,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_row_kernel(row_params p) 
     const int64_t end = PLACE == 2 ? a.tokens : min((block + 1) * kBlock, a.tokens);
     for (int64_t t0 = block * kBlock; t0 < end; t0 += kBlock) {
         const int64_t token = t0 + (tid >> 4);
-        const int expert = route_row<DT, BIASED, NE>(p, token, token < live, picks + (tid & ~15));
+        const int expert = route_row<DT, BIASED, NE>(p, token, token < live && token < a.tokens, picks + (tid & ~15));
         if constexpr (PLACE != 0) {
             if (l16 < a.top && token < a.tokens) chosen[int(token - block * kBlock) * a.top + l16] = int16_t(expert);
         }

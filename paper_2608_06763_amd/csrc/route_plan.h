@@ -10,6 +10,7 @@
 
 #include "cq_device.h"
 #include "experts_internal.h"
+#include "lane_scan.h"
 
 namespace cq {
 
@@ -90,25 +91,36 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
                 all[i] = p.table[int64_t(p.rows) * p.experts + e];
             }
         } else if (p.experts % 4 == 0) {
-            // four experts a thread; the slices' sums meet in LDS
+            // four experts a thread, of a slice of neighbouring rows; the slices' sums meet in
+            // LDS.  Most slices lie whole before this workgroup's rows, or behind.
             const int quads = p.experts / 4;
             slices = min(kPlanThreads / quads, 16);
-            const int s = tid / quads, e = 4 * (tid - s * quads);
+            const int s = tid / quads, e = 4 * (tid - s * quads), each = (p.rows + slices - 1) / slices;
             int4 some = make_int4(0, 0, 0, 0), early = some;
+            auto add = [](int4 &to, const int4 &c) {
+                to.x += c.x; to.y += c.y; to.z += c.z; to.w += c.w;
+            };
+            const int end_row = s < slices ? min((s + 1) * each, p.rows) : 0;
             constexpr int kTurn = 32;
-            for (int b0 = s; s < slices && b0 < p.rows; b0 += kTurn * slices) {
+            for (int b0 = s * each; b0 < end_row; b0 += kTurn) {
+                const int32_t *from = p.table + b0 * p.experts + e;
                 int4 c[kTurn];
 #pragma unroll
-                for (int i = 0; i < kTurn; ++i)
-                    c[i] = *reinterpret_cast<const int4 *>(p.table + min(b0 + i * slices, p.rows - 1) * p.experts + e);
-#pragma unroll
                 for (int i = 0; i < kTurn; ++i) {
-                    const int b = b0 + i * slices, in = b < p.rows, first = b < row0;
-                    some.x += in ? c[i].x : 0; some.y += in ? c[i].y : 0;
-                    some.z += in ? c[i].z : 0; some.w += in ? c[i].w : 0;
-                    early.x += first ? c[i].x : 0; early.y += first ? c[i].y : 0;
-                    early.z += first ? c[i].z : 0; early.w += first ? c[i].w : 0;
+                    c[i] = make_int4(0, 0, 0, 0);
+                    if (b0 + i < end_row) c[i] = *reinterpret_cast<const int4 *>(from);
+                    from += p.experts;
                 }
+                if (b0 < row0 && row0 < b0 + kTurn) {
+#pragma unroll
+                    for (int i = 0; i < kTurn; ++i)
+                        if (b0 + i < row0) add(early, c[i]);
+                }
+                int4 turn = make_int4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < kTurn; ++i) add(turn, c[i]);
+                add(some, turn);
+                if (b0 + kTurn <= row0) add(early, turn);
             }
             if (s < slices) {
                 *reinterpret_cast<int4 *>(sums + s * p.experts + e) = some;
@@ -155,12 +167,7 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
         sum += all[i];
     }
     // offsets of the experts: sums over the lanes of a wave, then over the waves
-    int upto = sum;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int v = __shfl_up(upto, d);
-        if (lane >= d) upto += v;
-    }
+    const int upto = wave_scan(sum);
     if (lane == 63) part[wave] = upto;
     __syncthreads();
     int at = upto - sum, total = 0;

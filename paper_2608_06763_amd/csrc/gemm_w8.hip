@@ -34,22 +34,32 @@ w8::params make(const cq_w8_args &a, bool routed) {
     return p;
 }
 
-// Time of a product in tiles, per stage of 128 codes of K and in units of 1 us: rounds over
-// 256 compute units by what a round's stage took on 28672 x 8192, 8192 x 8192 and 4096 x
-// 14336 (64 x 128 tiles wait for memory, 256 x 256 are bound by the matrix cores).
+// Time of a product in tiles, us: rounds over the workgroups that the card holds at once, by
+// what a round takes for its way in and out and for each stage of 128 codes of K, fitted to
+// 5302 x 9458 with 256 to 2048 codes, 2000 x 2000 with 256 to 4096, 8192 x 8192 and 256 x 28672
+// with 8192.  (64 x 128 tiles wait for memory, 256 x 256 are bound by the matrix cores; two
+// shallow 128 x 128 ones a compute unit hide each other's way in and out.  A single round of
+// those has other figures.)
 struct tile_t {
     int m, n;
-    double cost;
+    bool deep;
+    double slots, fixed, stage, fixed_alone, stage_alone;
 };
-constexpr tile_t kTiles[] = {{64, 128, 0.46}, {128, 128, 0.60}, {128, 256, 1.05}, {256, 256, 1.78}};
+constexpr tile_t kTiles[] = {{64, 128, true, 256, 3.0, 0.43, 3.0, 0.43},
+                             {128, 128, true, 256, 4.5, 0.57, 4.5, 0.57},
+                             {128, 128, false, 512, 4.8, 1.0, 3.0, 1.2},
+                             {128, 256, true, 256, 8.0, 1.08, 8.0, 1.08},
+                             {256, 256, true, 256, 12.0, 1.55, 12.0, 1.55}};
 
 hipError_t dense(const w8::params &p, hipStream_t stream) {
-    auto cells = [&](int m, int n) { return double((p.rows + m - 1) / m) * double((p.n + n - 1) / n); };
     if (p.rows <= 8) return w8::launch_few(p, false, stream);
+    auto cells = [&](int m, int n) { return double((p.rows + m - 1) / m) * double((p.n + n - 1) / n); };
+    const double stages = (p.k + 127) / 128;
     const tile_t *best = nullptr;
     double least = 0.0;
     for (const tile_t &t : kTiles) {
-        const double cost = std::ceil(cells(t.m, t.n) / 256.0) * t.cost;
+        const double rounds = std::ceil(cells(t.m, t.n) / t.slots);
+        const double cost = rounds == 1.0 ? t.fixed_alone + stages * t.stage_alone : rounds * (t.fixed + stages * t.stage);
         if (!best || cost < least) {
             best = &t;
             least = cost;
@@ -58,8 +68,8 @@ hipError_t dense(const w8::params &p, hipStream_t stream) {
     // Few rows of few channels: K shared out over a workgroup's waves, whose stage is a step
     // of each wave's eighth of K (45 rows of 4096 x 14336 19 us, in tiles 50; 48 of 14336 x
     // 4096 29 and 20).  Up to 16 rows that is the better kernel for all.
-    if (p.rows <= 16 || 0.2 * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::launch_rows(p, stream);
-    return w8::launch_wide(p, false, best->m, best->n, true, stream);
+    if (p.rows <= 16 || 1.0 + 0.2 * stages * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::launch_rows(p, stream);
+    return w8::launch_wide(p, false, best->m, best->n, best->deep, stream);
 }
 
 hipError_t routed(const w8::params &p, hipStream_t stream) {
@@ -71,14 +81,18 @@ hipError_t routed(const w8::params &p, hipStream_t stream) {
     // rows' kernel), 37 each 140 (64 x 256: 140), 62 each 162 (151); 64 experts of 4096 x
     // 4096: 62 each 292 (267; 128 x 256: 257), 250 each 469 in 128 x 256 (256 x 256: 473),
     // 500 each 753 (728).
-    const int m = each <= 80.0 ? 64 : each < 400.0 ? 128 : 256, n = each <= 40.0 ? 128 : 256;
+    // With short rows tiles that share a compute unit hide each other's way in and out.
+    const bool brief = p.k <= 1024 && each > 80.0;
+    const int m = each <= 80.0 ? 64 : each < 400.0 || brief ? 128 : 256, n = each <= 40.0 || brief ? 128 : 256;
     // a tile of each expert is half full, on average
     auto cells = [&](int tm, int tn) {
         return (double(p.routes) / tm + 0.5 * double(std::min<int64_t>(p.experts, p.routes))) * ((p.n + tn - 1) / tn);
     };
     if (cells(m, n) >= 256.0) return w8::launch_wide(p, true, m, n, false, stream);
-    const bool low = std::max(1.0, cells(64, 128) / 256.0) * kTiles[0].cost <= std::max(1.0, cells(128, 128) / 256.0) * kTiles[1].cost;
-    return w8::launch_wide(p, true, low ? 64 : 128, 128, true, stream);
+    // few tiles: the deeper ones, 64 or 128 rows high
+    const double stages = (p.k + 127) / 128;
+    auto cost = [&](const tile_t &t) { return std::max(1.0, cells(t.m, t.n) / t.slots) * (t.fixed + stages * t.stage); };
+    return w8::launch_wide(p, true, cost(kTiles[0]) <= cost(kTiles[1]) ? 64 : 128, 128, true, stream);
 }
 
 }  // namespace

@@ -8,7 +8,8 @@ namespace w8 {
 hipError_t launch_wide(const params &p, bool routed, int tile_m, int tile_n, bool deep, hipStream_t stream) {
     if (tile_m == 256) return routed ? wide_run<4, 4, 2, true>(p, stream) : wide_run<4, 4, 2, false>(p, stream);
     if (tile_m == 128 && tile_n == 256) return routed ? wide_run<2, 4, 3, true>(p, stream) : wide_run<2, 4, 3, false>(p, stream);
-    if (tile_m == 128) return routed ? wide_run<2, 2, 4, true>(p, stream) : wide_run<2, 2, 4, false>(p, stream);
+    if (tile_m == 128 && deep) return routed ? wide_run<2, 2, 4, true>(p, stream) : wide_run<2, 2, 4, false>(p, stream);
+    if (tile_m == 128) return routed ? wide_run<2, 2, 2, true>(p, stream) : wide_run<2, 2, 2, false>(p, stream);
     if (!routed) return wide_run<1, 2, 4, false>(p, stream);
     if (deep) return wide_run<1, 2, 4, true>(p, stream);
     return tile_n == 256 ? wide_run<1, 4, 2, true>(p, stream) : wide_run<1, 2, 2, true>(p, stream);

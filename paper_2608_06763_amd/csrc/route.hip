@@ -5,10 +5,11 @@
 // lanes a group of experts, so that four tokens share every instruction of a wave.
 //
 // Keys are the logits themselves without a bias (the order of the scores is theirs),
-// else the choices c_e = s_e + b_e in FP64: of 8192 tokens over 256 experts some always
-// have neighbours closer than FP32 tells apart.  FP64 keys of all experts and a search
-// of all for each choice took 12 us for 8191 tokens, bound by the latency of one wave's
-// instructions; FP32 keys find the few candidates, and FP64 orders those.
+// else the choices c_e = s_e + b_e in FP64: of 8191 tokens over 256 experts some 125 have
+// neighbours closer than 2^-22 somewhere in their order, up to two among the first nine, and
+// FP32 orders the first eight of one token in another way in two inputs of twelve.  FP64 keys
+// of all experts and a search of all for each choice took 12 us for 8191 tokens, bound by the
+// latency of one wave's instructions; FP32 keys find the few candidates, and FP64 orders those.
 //
 // Bound by the latency of a wave's instructions and of a chain of loads; the logits are
 // read once.  The tokens of a workgroup are counted by expert on the way, so that one more

@@ -134,7 +134,7 @@ ROUTES = [
 @pytest.mark.parametrize("tokens,experts,top", [(1, 1, 1), (1, 8, 2), (3, 7, 7), (1, 128, 8), (5, 60, 4), (70, 64, 6),
                                                 (130, 65, 1), (33, 160, 32), (700, 256, 8), (9, 384, 12), (17, 1000, 10),
                                                 (2, 1024, 32), (1500, 40, 3), (64, 512, 15),
-                                                (65, 512, 15), (65, 512, 16), (32, 513, 8), (33, 240, 9), (2000, 128, 2)])
+                                                (65, 512, 15), (65, 512, 16), (32, 513, 8), (33, 240, 9), (2000, 128, 2), (17000, 12, 2)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_route(torch_dev, tokens, experts, top, dtype):
     torch = torch_dev

@@ -89,9 +89,9 @@ __device__ __forceinline__ float raw_weight(const cq_route_args &a, int expert, 
 
 // ---------------------------------------------------------------- one wave a token
 
-// Lane j's expert, -1 for none; the weights are written.  NE experts a lane.
+// Lane j finds and writes the token's choice j and its weight.  NE experts a lane.
 template <int DT, typename K, int NE>
-__device__ __forceinline__ int route_wave(const cq_route_args &a, int64_t token) {
+__device__ __forceinline__ void route_wave(const cq_route_args &a, int64_t token) {
     const int lane = threadIdx.x & 63;
     const int64_t row = token * a.stride;
     float l[NE], b[NE];
@@ -196,7 +196,6 @@ __device__ __forceinline__ int route_wave(const cq_route_args &a, int64_t token)
         a.chosen[token * a.top + lane] = expert;
         a.weights[token * a.top + lane] = expert >= 0 ? w * a.scale : 0.f;
     }
-    return expert;
 }
 
 template <int DT, typename K, int NE>

@@ -149,7 +149,8 @@ def test_route(torch_dev, tokens, experts, top, dtype):
 
 @pytest.mark.parametrize("experts,groups,kept,top", [(8, 2, 1, 3), (16, 8, 3, 6), (64, 8, 4, 8), (256, 8, 4, 8),
                                                      (160, 5, 2, 6), (100, 50, 20, 12), (64, 64, 9, 9), (1024, 16, 3, 32),
-                                                     (60, 4, 3, 5), (512, 4, 4, 10), (72, 8, 1, 9), (64, 4, 1, 20)])
+                                                     (60, 4, 3, 5), (512, 4, 4, 10), (72, 8, 1, 9), (16, 16, 5, 5),
+                                                     (5, 5, 2, 2), (64, 4, 1, 20)])
 @pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
 def test_route_groups(torch_dev, experts, groups, kept, top, scoring):
     # the last one keeps fewer experts than it asks for

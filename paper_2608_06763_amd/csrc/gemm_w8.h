@@ -10,6 +10,7 @@
 
 #include "experts_internal.h"
 #include "lane_scan.h"
+#include "plan_run.h"
 #include "wide_common.h"
 
 namespace cq {
@@ -39,30 +40,28 @@ struct place {
 };
 
 // Tile t of the plan's routes.  Every lane of the wave takes part; the result is
-// wave-uniform.  Offsets are cut to the routes that there are.
+// wave-uniform.  Whatever the offsets hold, a tile lies inside the routes that there are
+// (plan_run.h): counts of tiles may wrap where runs overlap, a place inside a run is
+// checked against the run.
 __device__ __forceinline__ place find_tile(const params &p, int t, int tile) {
     const int lane = threadIdx.x & 63;
     place at = {0, 0, 0};
-    int before = 0;
+    uint32_t before = 0;
     for (int e0 = 0; e0 < p.experts; e0 += kWave) {
         const int e = e0 + lane;
-        int lo = 0, n = 0;
-        if (e < p.experts) {
-            lo = max(p.plan[e], 0);
-            n = max(min(p.plan[e + 1], int(p.routes)) - lo, 0);
-        }
-        const int tiles = (n + tile - 1) / tile;
-        const int upto = wave_scan(tiles);
-        const int mine = t - before - (upto - tiles);
-        const uint64_t found = __ballot(mine >= 0 && mine < tiles);
+        plan_run run = {0, 0};
+        if (e < p.experts) run = run_of(p.plan[e], p.plan[e + 1], int(p.routes));
+        const uint32_t tiles = tiles_of(run, tile), upto = wave_scan(tiles);
+        const uint32_t mine = uint32_t(t) - before - (upto - tiles);
+        const uint64_t found = __ballot(mine < tiles);
         if (found) {
             const int src = __builtin_ctzll(found);
-            at.expert = e0 + src;
-            at.first = __builtin_amdgcn_readlane(lo + mine * tile, src);
-            at.count = __builtin_amdgcn_readlane(min(n - mine * tile, tile), src);
+            const plan_run its = {__builtin_amdgcn_readlane(run.first, src), __builtin_amdgcn_readlane(run.count, src)};
+            const plan_run one = tile_of(its, uint32_t(__builtin_amdgcn_readlane(int(mine), src)), tile);
+            at = {e0 + src, one.first, one.count};
             break;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
+        before += uint32_t(__builtin_amdgcn_readlane(int(upto), 63));
     }
     return at;
 }

@@ -167,7 +167,7 @@ __device__ __forceinline__ void plan_place(const plan_params &p, int block, int6
         sum += all[i];
     }
     // offsets of the experts: sums over the lanes of a wave, then over the waves
-    const int upto = wave_scan(sum);
+    const int upto = int(wave_scan(uint32_t(sum)));
     if (lane == 63) part[wave] = upto;
     __syncthreads();
     int at = upto - sum, total = 0;

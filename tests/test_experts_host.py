@@ -2,6 +2,9 @@
 argument is refused, by its status, before any device work."""
 import contextlib
 import ctypes
+import os
+import random
+import subprocess
 
 import pytest
 
@@ -257,3 +260,55 @@ def test_arguments_of_other_shapes_and_types_are_refused(monkeypatch):
             call()
     with pytest.raises(ValueError):
         cq.cq_route(f.double(), 2)
+
+
+# ---------------------------------------------------------------- offsets of a plan
+
+_RUNS = """
+#include "plan_run.h"
+extern "C" void runs(int n, const int32_t *from, const int32_t *to, int32_t routes, int tile, int64_t *out) {
+    for (int i = 0; i < n; ++i) {
+        const cq::plan_run run = cq::run_of(from[i], to[i], routes);
+        const uint32_t tiles = cq::tiles_of(run, tile);
+        int64_t *o = out + 7 * i;
+        o[0] = run.first; o[1] = run.count; o[2] = tiles;
+        const cq::plan_run first = cq::tile_of(run, 0, tile), last = cq::tile_of(run, tiles ? tiles - 1 : 0, tile);
+        o[3] = first.first; o[4] = first.count; o[5] = last.first; o[6] = last.count;
+    }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def runs(tmp_path_factory):
+    """The kernels' own arithmetic of a plan's offsets, with signed overflow an error."""
+    where = tmp_path_factory.mktemp("plan_run")
+    (where / "runs.cpp").write_text(_RUNS)
+    csrc = os.path.join(os.path.dirname(cq.__file__), "csrc")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-ftrapv", "-shared", "-fPIC", "-I", csrc, "-o",
+                           str(where / "runs.so"), str(where / "runs.cpp")])
+    call = ctypes.CDLL(str(where / "runs.so")).runs
+
+    def run(pairs, routes, tile):
+        n, words = len(pairs), ctypes.c_int32 * len(pairs)
+        out = (ctypes.c_int64 * (7 * n))()
+        call(n, words(*(a for a, _ in pairs)), words(*(b for _, b in pairs)), routes, tile, out)
+        return [tuple(out[7 * i:7 * i + 7]) for i in range(n)]
+    return run
+
+
+@pytest.mark.parametrize("tile", [16, 64, 128, 256])
+@pytest.mark.parametrize("routes", [1, 2, 299, 300, 8191, 2**29])
+def test_no_offsets_of_a_plan_lead_outside_its_routes(runs, routes, tile):
+    far, rng = 2**31, random.Random(routes + tile)
+    odd = {0, 1, 5, 16, 255, 256, 257, routes - 1, routes, routes + 1, 2 * routes, far - 1, far - 2, far - 300}
+    odd = sorted({v for o in odd for v in (o, -o, -o - 1) if -far <= v < far})
+    pairs = [(a, b) for a in odd for b in odd]
+    pairs += [(rng.randrange(-far, far), rng.randrange(-far, far)) for _ in range(2000)]
+    pairs += [(rng.randrange(0, routes + 2), rng.randrange(-far, -far + routes + 2)) for _ in range(2000)]
+    for (a, b), (first, count, tiles, *ends) in zip(pairs, runs(pairs, routes, tile)):
+        lo, hi = (min(max(v, 0), routes) for v in (a, b))
+        assert (first, count, tiles) == (lo, max(hi - lo, 0), -(-max(hi - lo, 0) // tile)), (a, b)
+        if tiles:
+            last = lo + (tiles - 1) * tile
+            assert ends == [lo, min(tile, hi - lo), last, hi - last] and 0 <= last < hi <= routes, (a, b)

@@ -715,3 +715,26 @@ def test_decoder_block_example_with_experts(torch_dev):
     # carriers are off by up to half a step, 1 / 254 of a row's largest value, which for
     # products of two normal values is up to some fifteen times their root mean square
     assert len(errors) == 2 * 5 and max(errors) < 15.0 / 254.0 + 2.0**-7
+
+
+@pytest.mark.parametrize("experts,routes,n,k", [(5, 20, 40, 64), (70, 300, 40, 64), (5, 300, 40, 64), (16, 1000, 300, 144),
+                                                (8, 4000, 400, 144), (48, 16000, 300, 1040), (8, 32000, 300, 1040)])
+def test_offsets_far_from_each_other_lead_nowhere(torch_dev, experts, routes, n, k):
+    # neighbours of a plan whose difference passes 32 bits, by kernels with tiles of 16 to
+    # 256 rows: the routes of the runs that lie in the plan are written, and nothing else
+    torch, cq = torch_dev, _cq()
+    x8, dx = _int8(torch, 1, routes // 2, k), _scales(torch, 2, routes // 2)
+    w8, dw = _int8(torch, 3, experts, n, k), _scales(torch, 4, experts, n)
+    room = torch.full((routes + 40, n), 77.0, dtype=torch.bfloat16, device="cuda")
+    most, order = 2**31 - 1, list(range(routes))
+    for high, low in ((routes, -most), (most, -5), (most, -most - 1), (most, -most + routes // 2), (routes // 2 + 1, -most)):
+        for rest, runs in (([low] * (experts - 1), ()), ([3] + [9] * (experts - 2), ((0, 3, 1), (3, 9, 2)))):
+            say("offsets", experts, routes, n, k, high, low, len(runs))
+            plan = torch.tensor([high, low] + rest + order, dtype=torch.int32, device="cuda")
+            want = room.fill_(77.0).clone()
+            for first, end, e in runs:
+                r = torch.arange(first, end, device="cuda") // 2
+                want[20 + first:20 + end] = cq.cq_gemm_w8(x8[r], dx[r], w8[e], dw[e])
+            cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=2, out=room[20:20 + routes])
+            torch.cuda.synchronize()
+            assert torch.equal(room, want)

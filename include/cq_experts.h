@@ -83,7 +83,8 @@ cq_status cq_route_plan(const int32_t *chosen, int64_t routes, int32_t experts, 
 /*
  * cq_gemm_w8 -- product of 8-bit integers with a scale for each token and each
  * channel (device):  y_ij = dx_i dw_j sum_k x8_ik w8_jk + bias_j,
- * the sum exact in INT32, the rest FP32.  x8 and dx are what cq_quantize_act_a8
+ * the sum exact in INT32; in FP32 then dx_i dw_j, and its product with the sum and the
+ * bias in one multiply-add.  x8 and dx are what cq_quantize_act_a8
  * and cq_norm_residual_a8 make (dx_i here, d_x there); any int8 values are legal.
  *
  * cq_gemm_routed_w8 -- the same of routed experts: for every route r of the plan,

@@ -143,7 +143,9 @@ __device__ __forceinline__ void store4(void *y, int64_t to, const float *v, int 
         if (e < count) store_out<YDT>(y, to + e, v[e]);
 }
 
-// Outputs of four channels n .. n + 3 (those below p.n) of one row.
+// Outputs of four channels n .. n + 3 (those below p.n) of one row.  The bias comes in by the
+// multiply-add that the tiles' outputs take too (store_tile), so that every kernel gives the
+// same bits.
 template <int YDT>
 __device__ __forceinline__ void finish4(const params &p, const i32x4 &sum, float dx, int expert, int64_t row, int n) {
     if (n >= p.n) return;
@@ -153,8 +155,8 @@ __device__ __forceinline__ void finish4(const params &p, const i32x4 &sum, float
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (e < count) {
-            v[e] = float(sum[e]) * (dx * p.dw[channel + e]);
-            if (p.bias) v[e] += load_bias<YDT>(p.bias, channel + e);
+            const float b = p.bias ? load_bias<YDT>(p.bias, channel + e) : 0.f;
+            v[e] = __builtin_fmaf(float(sum[e]), dx * p.dw[channel + e], b);
         }
     store4<YDT>(p.y, row * p.n + n, v, count);
 }

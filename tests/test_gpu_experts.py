@@ -738,3 +738,21 @@ def test_offsets_far_from_each_other_lead_nowhere(torch_dev, experts, routes, n,
             cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=2, out=room[20:20 + routes])
             torch.cuda.synchronize()
             assert torch.equal(room, want)
+
+
+@pytest.mark.parametrize("n,k", [(700, 272), (6144, 400), (4099, 2064)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_product_with_a_bias_does_not_depend_on_the_kernel(torch_dev, n, k, dtype):
+    # a row has the same bits whichever rows come with it, dense or routed
+    torch, cq = torch_dev, _cq()
+    x8, dx = _int8(torch, 1, 2500, k), _scales(torch, 2, 2500)
+    w8, dw = _int8(torch, 3, 3, n, k), _scales(torch, 4, 3, n)
+    bias, out = _rand(torch, 5, 3, n, dtype=dtype, scale=3.0), dict(y_dtype=_dtype(torch, dtype))
+    one, done, bone = w8[1].clone(), dw[1].clone(), bias[1].clone()
+    want = cq.cq_gemm_w8(x8, dx, one, done, bias=bone, **out)
+    for rows in (1, 7, 9, 16, 17, 45, 100, 300, 700, 1300):
+        say("bias", n, k, dtype, rows)
+        got = cq.cq_gemm_w8(x8[:rows], dx[:rows], one, done, bias=bone, **out)
+        assert torch.equal(got, want[:rows]), rows
+        plan = cq.cq_route_plan(torch.ones((rows,), dtype=torch.int32, device="cuda"), 3)
+        assert torch.equal(cq.cq_gemm_routed_w8(x8[:rows], dx[:rows], w8, dw, plan, bias=bias, **out), got), rows

@@ -549,7 +549,9 @@ __device__ __forceinline__ bool choose_quick(const row_params &p, const row_t<NE
         merge_group(p, ghi, glo);
         float value = ghi, off = eps + fabsf(ghi) * 0x1p-23f;
         if (a.group_top == 2 && glo > lowest<float>()) {
-            value += glo;
+            // two of FP32's lowest have a sum in FP64 and none here: the infinite error that
+            // goes with it leaves the choice to the exact keys
+            value = fmaxf(value + glo, -3.402823466e38f);
             off += eps + (fabsf(glo) + fabsf(value)) * 0x1p-23f;
         }
         bool kept = group_kept(p, value, t.group_lane) && value > lowest<float>();

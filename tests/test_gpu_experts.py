@@ -756,3 +756,42 @@ def test_product_with_a_bias_does_not_depend_on_the_kernel(torch_dev, n, k, dtyp
         assert torch.equal(got, want[:rows]), rows
         plan = cq.cq_route_plan(torch.ones((rows,), dtype=torch.int32, device="cuda"), 3)
         assert torch.equal(cq.cq_gemm_routed_w8(x8[:rows], dx[:rows], w8, dw, plan, bias=bias, **out), got), rows
+
+
+@pytest.mark.parametrize("experts,groups", [(64, 8), (40, 5), (256, 16), (240, 3), (96, 32)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_route_of_groups_masked_by_the_lowest_bias(torch_dev, experts, groups, scoring):
+    # a bias of FP32's lowest value is a choice like others: behind all that are not masked,
+    # but in the group's sum of two beyond FP32
+    torch = torch_dev
+    size, low = experts // groups, torch.finfo(torch.float32).min
+    for n, masked in enumerate([range(groups), range(1, groups), range(0, groups - 1), range(0, groups, 2)]):
+        bias = _rand(torch, 90 + n, experts, dtype="fp32", scale=0.1)
+        for g in masked:
+            bias[g * size:(g + 1) * size] = low
+        if n == 3:  # one that is not masked in a masked group
+            bias[size // 2] = 0.25
+        logits = _rand(torch, 95 + n, 33, experts, dtype="fp32", scale=2.0)
+        for kept, top in ((1, 3), (2, 12), (min(groups - 1, 3), 4), (2, 16)):
+            for group_top in (1, 2):
+                say("masked groups", experts, groups, scoring, n, kept, top, group_top)
+                _check_route(torch, logits, top, (n, kept, top, group_top), scoring=scoring, bias=bias, groups=groups,
+                             kept_groups=kept, group_top=group_top)
+
+
+@pytest.mark.parametrize("experts,groups,top", [(64, 8, 8), (256, 16, 12), (240, 3, 5), (96, 1, 8), (512, 4, 16), (600, 50, 7)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_route_of_the_largest_biases(torch_dev, experts, groups, top, scoring):
+    # so large that scores vanish beside them, in FP64 too, and sums pass FP32
+    torch = torch_dev
+    most, inf = torch.finfo(torch.float32).max, float("inf")
+    kinds = torch.tensor([most, -most, 2e38, -2e38, 1e30, -1e30, 0.0, 0.5, inf, -inf, float("nan"), -0.0])
+    for seed in range(12):
+        g = torch.Generator().manual_seed(seed)
+        some = kinds[torch.randperm(len(kinds), generator=g)[:2 + seed % 4]]
+        bias = some[torch.randint(0, len(some), (experts,), generator=g)].cuda()
+        logits = _rand(torch, seed, 19, experts, dtype="fp32", scale=2.0)
+        for kept, group_top in ((1, 1), (1, 2), (2, 2)):
+            say("largest biases", experts, groups, top, scoring, seed, kept, group_top)
+            _check_route(torch, logits, top, (seed, some), scoring=scoring, bias=bias, groups=groups,
+                         kept_groups=min(kept, groups), group_top=group_top)

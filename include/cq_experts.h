@@ -37,12 +37,12 @@ typedef enum { CQ_ACT_SILU = 0, CQ_ACT_GELU_TANH = 1 } cq_activation;
  * group_top highest c_e (of its scores without a bias), and only experts of the
  * kept_groups groups with the highest values are chosen.  The weights are the
  * chosen s_e (without the bias), divided by their sum if renormalize (where the
- * sum is zero, as they are), times scale.  Where fewer than `top` experts can be
- * chosen the rest is expert -1 with weight 0, and so is all of a token at or
- * behind live[0].
+ * sum is zero, as they are: of sigmoids of logits below -745), times scale.  Where
+ * fewer than `top` experts can be chosen the rest is expert -1 with weight 0, and so
+ * is all of a token at or behind live[0].
  *
  * c_e is compared as in FP64, so that the choice does not depend on how a sum is
- * rounded; weights are FP32.
+ * rounded; weights are FP32, and quotients of scores that FP32 does not reach too.
  */
 typedef struct {
     const void *logits;      /* device, [tokens, experts] in dtype, token i at

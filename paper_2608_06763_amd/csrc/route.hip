@@ -79,12 +79,19 @@ __device__ __forceinline__ T relative_exp(T l, T m) {
 
 // Weight of a chosen expert (or -1) with logit l: before the division by their sum.
 // most, total: of all of the token's logits.
+//
+// A softmax's are relative to the highest chosen, which cancels in the quotient.  So are
+// those of a sigmoid, e^l / (1 + e^l) for l < 0, where the highest is below e^-16: from there
+// on FP32's least values, e^-87 and less, would lose what counts beside it.  (Above, all that
+// is lost is below 2^-126 of the sum.)  Below e^-745 a score is zero in FP64 too.
 __device__ __forceinline__ float raw_weight(const cq_route_args &a, int expert, float l, float most_chosen, float most,
                                             float total) {
     if (expert < 0) return 0.f;
     if (a.scoring == CQ_SCORE_SOFTMAX)
         return a.renormalize ? relative_exp<float>(l, most_chosen) : relative_exp<float>(l, most) / total;
-    return 1.f / (1.f + expf(-l));
+    if (l >= 0.f) return 1.f / (1.f + expf(-l));
+    const float from = a.renormalize && most_chosen < -16.f ? most_chosen : 0.f;
+    return most_chosen < -745.f ? 0.f : expf(l - from) / (1.f + expf(l));
 }
 
 // ---------------------------------------------------------------- one wave a token

@@ -795,3 +795,23 @@ def test_route_of_the_largest_biases(torch_dev, experts, groups, top, scoring):
             say("largest biases", experts, groups, top, scoring, seed, kept, group_top)
             _check_route(torch, logits, top, (seed, some), scoring=scoring, bias=bias, groups=groups,
                          kept_groups=min(kept, groups), group_top=group_top)
+
+
+@pytest.mark.parametrize("low,high", [(-150.0, -89.0), (-115.0, -60.0), (-40.0, -5.0), (-700.0, -650.0), (-17.0, -15.0)])
+@pytest.mark.parametrize("experts,top,groups", [(40, 6, 1), (256, 8, 8), (100, 20, 1), (64, 4, 32)])
+def test_route_of_sigmoids_that_all_vanish(torch_dev, low, high, experts, top, groups):
+    # scores below FP32's range have a sum to be divided by all the same
+    torch = torch_dev
+    g = torch.Generator().manual_seed(experts)
+    logits = (low + (high - low) * torch.rand((37, experts), generator=g)).cuda()
+    bias = _rand(torch, 9, experts, dtype="fp32", scale=0.1)
+    for b in (None, bias):
+        say("vanishing", low, high, experts, top, b is not None)
+        _, weights, _ = _check_route(torch, logits, top, (low, b is None), scoring="sigmoid", bias=b, groups=groups,
+                                     kept_groups=max(1, groups // 2))
+        # each quotient and the sum of all are rounded
+        assert bool(((weights.double().sum(1) - 1.0).abs() < (top + 8) * E).all())
+    logits[::3, ::2] = -10.0  # beside scores that have not vanished
+    _check_route(torch, logits, top, "beside", scoring="sigmoid", bias=bias, groups=groups, kept_groups=max(1, groups // 2))
+    logits[5] = -2000.0  # FP64 has no such score
+    assert not bool(_cq().cq_route(logits, top, scoring="sigmoid")[1][5].any())

@@ -7,6 +7,7 @@
 #define CQ_MEASURE_H
 
 #include "cq.h"
+#include "cq_experts.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -30,6 +31,20 @@ cq_status cq_probe_read(const void *buf, int64_t bytes, uint32_t *sink, void *st
  * test states with it which heights its shapes run.
  */
 int32_t cq_probe_wide_rows(int32_t path, const cq_weight *w, int64_t m);
+
+/*
+ * cq_probe_w8_kernel -- kernel (cq_w8_kernel) that cq_gemm_w8, or cq_gemm_routed_w8 if
+ * routed is not 0, takes for these arguments; 0 where it refuses them.  tile: rows and
+ * channels of a workgroup, and the stages of K that it has in flight.  Host only: a test
+ * states with it which kernels its shapes run.
+ */
+typedef enum {
+    CQ_W8_FEW = 1,      /* operands straight into registers                      */
+    CQ_W8_ROWS = 2,     /* through LDS, K shared out over a workgroup's waves     */
+    CQ_W8_TILES = 3,    /* tiles that the waves of a workgroup share             */
+    CQ_W8_TILES_FAR = 4 /* the same for routed rows of x of 2 GiB and more       */
+} cq_w8_kernel;
+int32_t cq_probe_w8_kernel(const cq_w8_args *args, int32_t routed, int32_t *tile);
 
 #ifdef __cplusplus
 }

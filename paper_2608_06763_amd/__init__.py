@@ -11,8 +11,8 @@ Entry points (same names as the C ABI):
   cq_gemm_routed_model_dtype, cq_gemm_routed_model_dtype_noalloc, cq_set_gemv_max_rows, cq_get_gemv_max_rows,
   cq_set_a8_fused_launch, cq_get_a8_fused_launch,
   cq_family_supported, cq_gemm_model_dtype_family, cq_gemm_a8_family,
-  cq_select_set, cq_select_query, cq_probe_read and cq_probe_wide_rows (measurement aids,
-  include/cq_measure.h)
+  cq_select_set, cq_select_query, cq_probe_read, cq_probe_wide_rows and cq_probe_w8_kernel
+  (measurement aids, include/cq_measure.h)
 The operators between the packed products (norms, rotary append, paged
 attention; include/cq_block.h) are bound in ``block.py`` and exported here, and so
 are those of a mixture-of-experts layer (routing, 8-bit products, gated activation,
@@ -42,7 +42,7 @@ EXPORTS = ("cq_status_str", "cq_pack_groups", "cq_decode_ref", "cq_gemm_model_dt
            "cq_get_a8_fused_launch", "cq_probe_wide_rows", "cq_norm_residual", "cq_norm_residual_a8",
            "cq_rope_append", "cq_attn_paged", "cq_attn_shared_prefix", "cq_attn_workspace_bytes", "cq_route",
            "cq_route_workspace_bytes", "cq_route_plan", "cq_route_plan_workspace_bytes", "cq_gemm_w8",
-           "cq_gemm_routed_w8", "cq_gated", "cq_gated_a8", "cq_combine")
+           "cq_gemm_routed_w8", "cq_gated", "cq_gated_a8", "cq_combine", "cq_probe_w8_kernel")
 
 CQ_PATH_MODEL_DTYPE, CQ_PATH_A8 = 0, 1
 FAMILIES = {"auto": 0, "gemv_stream": 1, "gemv_lut": 2, "gemv_narrow": 3, "gemv_generic": 4, "gemm_mfma": 5,
@@ -478,6 +478,7 @@ from .experts import (  # noqa: E402,F401
     cq_gated_a8,
     cq_gemm_routed_w8,
     cq_gemm_w8,
+    cq_probe_w8_kernel,
     cq_route,
     cq_route_plan,
 )

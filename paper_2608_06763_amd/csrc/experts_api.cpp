@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "../../include/cq_measure.h"
 #include "experts_internal.h"
 
 namespace {
@@ -48,7 +49,7 @@ cq_status check_plan(int64_t routes, int32_t experts) {
     return CQ_OK;
 }
 
-cq_status w8(const cq_w8_args *a, bool routed, void *stream) {
+cq_status check_w8(const cq_w8_args *a, bool routed) {
     if (!a || !a->x8 || !a->dx || !a->w8 || !a->dw || !a->y || a->rows < 1 || a->n < 1 || a->k < 1) return CQ_ERR_ARG;
     if (routed && (!a->plan || a->routes < 1 || a->experts < 1 || a->fan < 1)) return CQ_ERR_ARG;
     if (!routed && (a->plan || a->routes || a->experts || a->fan)) return CQ_ERR_ARG;
@@ -65,8 +66,12 @@ cq_status w8(const cq_w8_args *a, bool routed, void *stream) {
         !aligned16(a->y))
         return CQ_ERR_ALIGN;
     if (!aligned4(a->plan)) return CQ_ERR_ALIGN;
-    if (!cq::w8_fits(*a, routed)) return CQ_ERR_SHAPE;
-    return hip_status(cq::launch_gemm_w8(*a, routed, static_cast<hipStream_t>(stream)));
+    return cq::w8_fits(*a, routed) ? CQ_OK : CQ_ERR_SHAPE;
+}
+
+cq_status w8(const cq_w8_args *a, bool routed, void *stream) {
+    const cq_status st = check_w8(a, routed);
+    return st != CQ_OK ? st : hip_status(cq::launch_gemm_w8(*a, routed, static_cast<hipStream_t>(stream)));
 }
 
 cq_status check_gated(const cq_gated_args *a) {
@@ -114,6 +119,10 @@ cq_status cq_route_plan(const int32_t *chosen, int64_t routes, int32_t experts, 
 cq_status cq_gemm_w8(const cq_w8_args *args, void *stream) { return w8(args, false, stream); }
 
 cq_status cq_gemm_routed_w8(const cq_w8_args *args, void *stream) { return w8(args, true, stream); }
+
+int32_t cq_probe_w8_kernel(const cq_w8_args *args, int32_t routed, int32_t *tile) {
+    return tile && check_w8(args, routed != 0) == CQ_OK ? cq::w8_kernel(*args, routed != 0, tile) : 0;
+}
 
 cq_status cq_gated(const cq_gated_args *args, void *stream) {
     const cq_status st = check_gated(args);

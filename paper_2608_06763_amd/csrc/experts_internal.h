@@ -17,6 +17,7 @@ hipError_t launch_route_plan(const int32_t *chosen, int64_t routes, int experts,
 
 // routed: with a plan; whether a launch holds the call's workgroups
 bool w8_fits(const cq_w8_args &a, bool routed);
+int w8_kernel(const cq_w8_args &a, bool routed, int32_t *tile);  // cq_probe_w8_kernel
 hipError_t launch_gemm_w8(const cq_w8_args &a, bool routed, hipStream_t stream);
 
 hipError_t launch_gated(const cq_gated_args &a, int8_t *x8, float *dx, hipStream_t stream);

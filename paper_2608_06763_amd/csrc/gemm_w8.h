@@ -8,6 +8,7 @@
 // q = l / 16 the codes 32 q .. +31 (any order of K does, being the same for both operands).
 #pragma once
 
+#include "../../include/cq_measure.h"
 #include "experts_internal.h"
 #include "lane_scan.h"
 #include "plan_run.h"
@@ -161,11 +162,21 @@ __device__ __forceinline__ void finish4(const params &p, const i32x4 &sum, float
     store4<YDT>(p.y, row * p.n + n, v, count);
 }
 
-hipError_t launch_few(const params &p, bool routed, hipStream_t stream);
-hipError_t launch_rows(const params &p, hipStream_t stream);
-// tiles of tile_m rows by tile_n channels: 64 x 128, 64 x 256, 128 x 128, 128 x 256 or
-// 256 x 256; deep: more stages in flight, one workgroup on a compute unit
-hipError_t launch_wide(const params &p, bool routed, int tile_m, int tile_n, bool deep, hipStream_t stream);
+// Kernel of a call: its tile of rows by channels, and the stages (of few rows: a wave's
+// steps) that are in flight at a time.
+struct choice {
+    int kind;  // cq_w8_kernel
+    int height, width, depth;
+};
+
+// few rows: `width` says how many of the workgroup's waves share out K
+choice few_rows_choice(const params &p, bool routed);
+choice rows_choice(const params &p);
+hipError_t launch_few(const params &p, bool routed, const choice &c, hipStream_t stream);
+hipError_t launch_rows(const params &p, const choice &c, hipStream_t stream);
+// tiles of 64 x 128, 64 x 256, 128 x 128, 128 x 256 or 256 x 256; with four stages in
+// flight, or three of 128 x 256, one workgroup on a compute unit
+hipError_t launch_wide(const params &p, bool routed, const choice &c, hipStream_t stream);
 // any size of the rows of x, routed
 hipError_t launch_wide_far(const params &p, hipStream_t stream);
 

@@ -41,24 +41,25 @@ w8::params make(const cq_w8_args &a, bool routed) {
 // shallow 128 x 128 ones a compute unit hide each other's way in and out.  A single round of
 // those has other figures.)
 struct tile_t {
-    int m, n;
-    bool deep;
+    int height, width, depth;
     double slots, fixed, stage, fixed_alone, stage_alone;
 };
-constexpr tile_t kTiles[] = {{64, 128, true, 256, 3.0, 0.43, 3.0, 0.43},
-                             {128, 128, true, 256, 4.5, 0.57, 4.5, 0.57},
-                             {128, 128, false, 512, 4.8, 1.0, 3.0, 1.2},
-                             {128, 256, true, 256, 8.0, 1.08, 8.0, 1.08},
-                             {256, 256, true, 256, 12.0, 1.55, 12.0, 1.55}};
+constexpr tile_t kTiles[] = {{64, 128, 4, 256, 3.0, 0.43, 3.0, 0.43},
+                             {128, 128, 4, 256, 4.5, 0.57, 4.5, 0.57},
+                             {128, 128, 2, 512, 4.8, 1.0, 3.0, 1.2},
+                             {128, 256, 3, 256, 8.0, 1.08, 8.0, 1.08},
+                             {256, 256, 2, 256, 12.0, 1.55, 12.0, 1.55}};
 
-hipError_t dense(const w8::params &p, hipStream_t stream) {
-    if (p.rows <= 8) return w8::launch_few(p, false, stream);
+w8::choice tiles(const tile_t &t) { return {CQ_W8_TILES, t.height, t.width, t.depth}; }
+
+w8::choice dense(const w8::params &p) {
+    if (p.rows <= 8) return w8::few_rows_choice(p, false);
     auto cells = [&](int m, int n) { return double((p.rows + m - 1) / m) * double((p.n + n - 1) / n); };
     const double stages = (p.k + 127) / 128;
     const tile_t *best = nullptr;
     double least = 0.0;
     for (const tile_t &t : kTiles) {
-        const double rounds = std::ceil(cells(t.m, t.n) / t.slots);
+        const double rounds = std::ceil(cells(t.height, t.width) / t.slots);
         const double cost = rounds == 1.0 ? t.fixed_alone + stages * t.stage_alone : rounds * (t.fixed + stages * t.stage);
         if (!best || cost < least) {
             best = &t;
@@ -68,15 +69,15 @@ hipError_t dense(const w8::params &p, hipStream_t stream) {
     // Few rows of few channels: K shared out over a workgroup's waves, whose stage is a step
     // of each wave's eighth of K (45 rows of 4096 x 14336 19 us, in tiles 50; 48 of 14336 x
     // 4096 29 and 20).  Up to 16 rows that is the better kernel for all.
-    if (p.rows <= 16 || 1.0 + 0.2 * stages * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::launch_rows(p, stream);
-    return w8::launch_wide(p, false, best->m, best->n, best->deep, stream);
+    if (p.rows <= 16 || 1.0 + 0.2 * stages * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::rows_choice(p);
+    return tiles(*best);
 }
 
-hipError_t routed(const w8::params &p, hipStream_t stream) {
-    if (p.rows * p.k >= int64_t(1) << 31) return w8::launch_wide_far(p, stream);
+w8::choice routed(const w8::params &p) {
+    if (p.rows * p.k >= int64_t(1) << 31) return {CQ_W8_TILES_FAR, 128, 128, 2};
     // routes of an expert, were all taken alike
     const double each = double(p.routes) / p.experts;
-    if (each <= 5.0) return w8::launch_few(p, true, stream);
+    if (each <= 5.0) return w8::few_rows_choice(p, true);
     // 128 experts of 2048 x 2048, us: 6 routes each 102 in tiles of 64 x 128 (109 by the few
     // rows' kernel), 37 each 140 (64 x 256: 140), 62 each 162 (151); 64 experts of 4096 x
     // 4096: 62 each 292 (267; 128 x 256: 257), 250 each 469 in 128 x 256 (256 x 256: 473),
@@ -88,12 +89,16 @@ hipError_t routed(const w8::params &p, hipStream_t stream) {
     auto cells = [&](int tm, int tn) {
         return (double(p.routes) / tm + 0.5 * double(std::min<int64_t>(p.experts, p.routes))) * ((p.n + tn - 1) / tn);
     };
-    if (cells(m, n) >= 256.0) return w8::launch_wide(p, true, m, n, false, stream);
+    if (cells(m, n) >= 256.0) return {CQ_W8_TILES, m, n, m == 128 && n == 256 ? 3 : 2};
     // few tiles: the deeper ones, 64 or 128 rows high
     const double stages = (p.k + 127) / 128;
-    auto cost = [&](const tile_t &t) { return std::max(1.0, cells(t.m, t.n) / t.slots) * (t.fixed + stages * t.stage); };
-    return w8::launch_wide(p, true, cost(kTiles[0]) <= cost(kTiles[1]) ? 64 : 128, 128, true, stream);
+    auto cost = [&](const tile_t &t) {
+        return std::max(1.0, cells(t.height, t.width) / t.slots) * (t.fixed + stages * t.stage);
+    };
+    return tiles(cost(kTiles[0]) <= cost(kTiles[1]) ? kTiles[0] : kTiles[1]);
 }
+
+w8::choice choose(const w8::params &p, bool with_routes) { return with_routes ? routed(p) : dense(p); }
 
 }  // namespace
 
@@ -103,9 +108,23 @@ bool w8_fits(const cq_w8_args &a, bool routed) {
     return tiles < (int64_t(1) << 23) / ((a.n + 127) / 128);
 }
 
+int w8_kernel(const cq_w8_args &a, bool with_routes, int32_t *tile) {
+    const w8::choice c = choose(make(a, with_routes), with_routes);
+    tile[0] = c.height;
+    tile[1] = c.width;
+    tile[2] = c.depth;
+    return c.kind;
+}
+
 hipError_t launch_gemm_w8(const cq_w8_args &a, bool with_routes, hipStream_t stream) {
     const w8::params p = make(a, with_routes);
-    return with_routes ? routed(p, stream) : dense(p, stream);
+    const w8::choice c = choose(p, with_routes);
+    switch (c.kind) {
+        case CQ_W8_FEW: return w8::launch_few(p, with_routes, c, stream);
+        case CQ_W8_ROWS: return w8::launch_rows(p, c, stream);
+        case CQ_W8_TILES: return w8::launch_wide(p, with_routes, c, stream);
+    }
+    return w8::launch_wide_far(p, stream);
 }
 
 }  // namespace cq

@@ -269,11 +269,10 @@ int sharing(int64_t blocks, int k) {
 }
 
 template <bool ROUTED>
-hipError_t few(const params &p, hipStream_t stream) {
-    const int64_t tiles = ROUTED ? most_tiles(p.routes, p.experts, 16) : (p.rows + 15) / 16;
-    switch (sharing(tiles * ((p.n + 15) / 16), p.k)) {
-        case 8: return run_few<8, ROUTED>(p, stream);
-        case 4: return run_few<4, ROUTED>(p, stream);
+hipError_t few(const params &p, int width, hipStream_t stream) {
+    switch (width) {
+        case 16: return run_few<8, ROUTED>(p, stream);
+        case 32: return run_few<4, ROUTED>(p, stream);
     }
     return run_few<2, ROUTED>(p, stream);
 }
@@ -282,13 +281,23 @@ hipError_t few(const params &p, hipStream_t stream) {
 
 namespace w8 {
 
-hipError_t launch_few(const params &p, bool routed, hipStream_t stream) {
-    return routed ? few<true>(p, stream) : few<false>(p, stream);
+choice few_rows_choice(const params &p, bool routed) {
+    const int64_t tiles = routed ? most_tiles(p.routes, p.experts, 16) : (p.rows + 15) / 16;
+    return {CQ_W8_FEW, 16, 16 * (kWaves / sharing(tiles * ((p.n + 15) / 16), p.k)), kAhead};
 }
 
-hipError_t launch_rows(const params &p, hipStream_t stream) {
-    if (p.rows <= 16) return sharing((p.n + 15) / 16, p.k) == 8 ? run_rows<1, 2, 8>(p, stream) : run_rows<1, 2, 4>(p, stream);
-    return run_rows<2, 2, 8>(p, stream);
+choice rows_choice(const params &p) {
+    if (p.rows > 16) return {CQ_W8_ROWS, 32, 32, kDepth<2, 2>};
+    return {CQ_W8_ROWS, 16, sharing((p.n + 15) / 16, p.k) == 8 ? 32 : 64, kDepth<1, 2>};
+}
+
+hipError_t launch_few(const params &p, bool routed, const choice &c, hipStream_t stream) {
+    return routed ? few<true>(p, c.width, stream) : few<false>(p, c.width, stream);
+}
+
+hipError_t launch_rows(const params &p, const choice &c, hipStream_t stream) {
+    if (c.height == 32) return run_rows<2, 2, 8>(p, stream);
+    return c.width == 32 ? run_rows<1, 2, 8>(p, stream) : run_rows<1, 2, 4>(p, stream);
 }
 
 }  // namespace w8

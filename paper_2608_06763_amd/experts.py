@@ -64,6 +64,8 @@ def declare(L):
                        ("cq_combine", [_vp, _vp])):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = args
+    L.cq_probe_w8_kernel.restype = _i32
+    L.cq_probe_w8_kernel.argtypes = [_vp, _i32, ctypes.POINTER(_i32)]
     for name, args in (("cq_route_workspace_bytes", [_vp]), ("cq_route_plan_workspace_bytes", [_i64, _i32])):
         getattr(L, name).restype = _i64
         getattr(L, name).argtypes = args
@@ -219,6 +221,18 @@ def cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=1, bias=None, y_dtype=None, out=
                     fan)
     _check(lib().cq_gemm_routed_w8(args, on), "cq_gemm_routed_w8")
     return out
+
+
+W8_KERNELS = (None, "few", "rows", "tiles", "tiles far")
+
+
+def cq_probe_w8_kernel(rows, n, k, experts=0, routes=0, fan=1):
+    """Kernel that a product of these sizes takes, routed if it has experts: (name, rows
+    and channels of a workgroup, stages in flight), or None where it is refused."""
+    at, tile = 4096, (_i32 * 3)()  # any aligned address: none is read
+    args = _W8.pack(at, at, at, at, 0, at, rows, n, k, 0, experts, at if experts else 0, routes, fan if experts else 0)
+    kernel = lib().cq_probe_w8_kernel(args, int(experts > 0), tile)
+    return (W8_KERNELS[kernel], *tile) if kernel else None
 
 
 # ---------------------------------------------------------------- between the products and behind them

@@ -101,3 +101,45 @@ def carrier_probe(bits: int, group: int, seed: int = 5):
     dx = np.full(1, 127.0, np.float32)
     _, p = A8.gemm_a8(x8, dx, codes, bits, group, s, a, b)
     return codes, s, a, b, x8, dx, p
+
+
+# Sizes of 8-bit products that reach every kernel, with the kernel that they take
+# (cq_probe_w8_kernel): rows, n, k; and experts, tokens, routes of a token, n, k.
+W8_DENSE = [
+    (5, 303, 144, ("few", 16, 16, 4)),
+    (7, 13003, 4112, ("few", 16, 32, 4)),
+    (3, 13001, 1040, ("few", 16, 64, 4)),
+    (13, 203, 400, ("rows", 16, 32, 3)),
+    (13, 13001, 144, ("rows", 16, 64, 3)),
+    (45, 303, 528, ("rows", 32, 32, 2)),
+    (300, 6144, 256, ("tiles", 64, 128, 4)),
+    (301, 6139, 272, ("tiles", 64, 128, 4)),
+    (260, 8001, 272, ("tiles", 128, 128, 4)),
+    (2500, 1001, 272, ("tiles", 128, 128, 4)),
+    (500, 6139, 144, ("tiles", 128, 128, 2)),
+    (1025, 3001, 144, ("tiles", 128, 128, 2)),
+    (700, 6144, 8192, ("tiles", 128, 256, 3)),
+    (701, 6133, 8208, ("tiles", 128, 256, 3)),
+    (1300, 6144, 1408, ("tiles", 256, 256, 2)),
+    (1301, 6137, 1424, ("tiles", 256, 256, 2)),
+    (2500, 4001, 1040, ("tiles", 256, 256, 2)),
+]
+W8_ROUTED = [
+    (64, 25, 8, 100, 272, ("few", 16, 16, 4)),
+    (64, 100, 3, 161, 4112, ("few", 16, 32, 4)),
+    (64, 100, 2, 3100, 272, ("few", 16, 64, 4)),
+    (48, 250, 4, 1001, 144, ("tiles", 64, 128, 2)),
+    (8, 75, 4, 4001, 144, ("tiles", 64, 128, 2)),
+    (16, 251, 4, 300, 144, ("tiles", 64, 128, 4)),
+    (96, 1500, 4, 301, 144, ("tiles", 64, 256, 2)),
+    (48, 667, 3, 2003, 144, ("tiles", 64, 256, 2)),
+    (3, 1001, 2, 2003, 144, ("tiles", 128, 128, 2)),
+    (32, 1000, 4, 1703, 400, ("tiles", 128, 128, 2)),
+    (16, 250, 4, 2048, 144, ("tiles", 128, 128, 4)),
+    (1, 16001, 1, 301, 1040, ("tiles", 128, 128, 4)),
+    (48, 4000, 4, 300, 1040, ("tiles", 128, 256, 3)),
+    (48, 1501, 4, 1001, 1040, ("tiles", 128, 256, 3)),
+    (8, 8000, 4, 300, 1040, ("tiles", 256, 256, 2)),
+    (8, 7999, 4, 309, 1040, ("tiles", 256, 256, 2)),
+    (3, 8001, 2, 1001, 1040, ("tiles", 256, 256, 2)),
+]

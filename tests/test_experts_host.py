@@ -10,6 +10,7 @@ import pytest
 
 import paper_2608_06763_amd as cq
 from paper_2608_06763_amd import experts as E
+from tests._cases import W8_DENSE, W8_ROUTED
 
 OK, BAD = 4096, 4100  # a 16-byte aligned address that nothing reads, and one that is not aligned
 ODD = 4097
@@ -312,3 +313,36 @@ def test_no_offsets_of_a_plan_lead_outside_its_routes(runs, routes, tile):
         if tiles:
             last = lo + (tiles - 1) * tile
             assert ends == [lo, min(tile, hi - lo), last, hi - last] and 0 <= last < hi <= routes, (a, b)
+
+
+# ---------------------------------------------------------------- kernels of the products
+
+
+def test_sizes_of_the_gpu_tests_take_every_kernel():
+    # a change of the choice must not leave one of them without a test unseen
+    taken = {False: {want for *_, want in W8_DENSE}, True: {want for *_, want in W8_ROUTED}}
+    for rows, n, k, want in W8_DENSE:
+        assert cq.cq_probe_w8_kernel(rows, n, k) == want, (rows, n, k)
+    for experts, tokens, top, n, k, want in W8_ROUTED:
+        for rows, fan in ((tokens, top), (tokens * top, 1)):
+            assert cq.cq_probe_w8_kernel(rows, n, k, experts, tokens * top, fan) == want, (experts, tokens, top, n, k)
+    few, tiles = {("few", 16, w, 4) for w in (16, 32, 64)}, {(128, 128, 2), (128, 128, 4), (128, 256, 3), (256, 256, 2)}
+    assert taken[False] == few | {("rows", 16, 32, 3), ("rows", 16, 64, 3), ("rows", 32, 32, 2)} | {
+        ("tiles", *t) for t in tiles | {(64, 128, 4)}}
+    assert taken[True] == few | {("tiles", *t) for t in tiles | {(64, 128, 2), (64, 128, 4), (64, 256, 2)}}
+    for rows in (1, 3, 8, 9, 16, 17, 40, 64, 65, 130, 300, 700, 1300, 3000, 8191):
+        for n in (1, 40, 300, 1001, 2003, 4096, 6144, 12001, 28672):
+            for k in (16, 144, 1040, 2064, 4112, 8192, 14336, 131056):
+                assert cq.cq_probe_w8_kernel(rows, n, k) in taken[False], (rows, n, k)
+                for experts in (1, 8, 48, 128, 1000):
+                    if rows * k < 1 << 31:
+                        assert cq.cq_probe_w8_kernel(rows, n, k, experts, rows) in taken[True], (rows, n, k, experts)
+
+
+def test_kernels_of_products_that_are_refused():
+    L, tile = cq.lib(), (ctypes.c_int32 * 3)()
+    assert cq.cq_probe_w8_kernel(5, 40, 17) is None and cq.cq_probe_w8_kernel(5, 40, 16, 4, 6, 1) is None
+    assert cq.cq_probe_w8_kernel(65536, 203, 32768, 5, 131072, 2) == ("tiles far", 128, 128, 2)
+    assert cq.cq_probe_w8_kernel(65535, 203, 32768, 5, 131070, 2)[0] == "tiles"
+    assert L.cq_probe_w8_kernel(None, 0, tile) == 0 and L.cq_probe_w8_kernel(ref(product()), 0, None) == 0
+    assert L.cq_probe_w8_kernel(ref(product()), 0, tile) == 2 and L.cq_probe_w8_kernel(ref(product()), 1, tile) == 0

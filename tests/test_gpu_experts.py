@@ -7,7 +7,7 @@ Chosen experts, plans, INT32 sums and carriers are exact.
 import numpy as np
 import pytest
 
-from tests._cases import say
+from tests._cases import W8_DENSE, W8_ROUTED, say
 
 pytestmark = pytest.mark.gpu
 
@@ -815,3 +815,48 @@ def test_route_of_sigmoids_that_all_vanish(torch_dev, low, high, experts, top, g
     _check_route(torch, logits, top, "beside", scoring="sigmoid", bias=bias, groups=groups, kept_groups=max(1, groups // 2))
     logits[5] = -2000.0  # FP64 has no such score
     assert not bool(_cq().cq_route(logits, top, scoring="sigmoid")[1][5].any())
+
+
+@pytest.mark.parametrize("rows,n,k,kernel", W8_DENSE)
+def test_product_by_every_kernel(torch_dev, rows, n, k, kernel):
+    torch, cq = torch_dev, _cq()
+    assert cq.cq_probe_w8_kernel(rows, n, k) == kernel
+    x8, w8 = _int8(torch, rows + k, rows, k), _int8(torch, n + k, n, k)
+    dx, dw = _scales(torch, 1, rows), _scales(torch, 2, n)
+    for dtype in ("bf16", "fp16", "fp32"):
+        for biased in (False, True):
+            say("product by", kernel, rows, n, k, dtype, biased)
+            bias = _rand(torch, 3, n, dtype=dtype) if biased else None
+            # what lies before and behind the output stays
+            room = torch.full((rows * n + 128,), 7.0, dtype=_dtype(torch, dtype), device="cuda")
+            got = cq.cq_gemm_w8(x8, dx, w8, dw, bias=bias, out=room[64:64 + rows * n].view(rows, n))
+            _check_on_device(torch, got, x8, dx, w8, dw, bias, dtype, (kernel, dtype, biased))
+            assert bool((room[:64] == 7.0).all()) and bool((room[64 + rows * n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("experts,tokens,top,n,k,kernel", W8_ROUTED)
+@pytest.mark.parametrize("fan", [True, False])
+def test_routed_product_by_every_kernel(torch_dev, experts, tokens, top, n, k, kernel, fan):
+    torch, cq = torch_dev, _cq()
+    g = torch.Generator().manual_seed(experts * tokens)
+    rows, per = (tokens, top) if fan else (tokens * top, 1)
+    assert cq.cq_probe_w8_kernel(rows, n, k, experts, tokens * top, per) == kernel
+    w8, dw = _int8(torch, 1, experts, n, k), _scales(torch, 2, experts, n)
+    x8, dx = _int8(torch, 3, rows, k), _scales(torch, 4, rows)
+    # some experts far more in demand than others, some routes of none
+    chosen = (torch.rand((tokens, top), generator=g) ** 2 * (experts + 0.3)).long() - (torch.rand((tokens, top), generator=g) < 0.1).long()
+    flat = chosen.flatten().cuda()
+    plan = cq.cq_route_plan(chosen.to(torch.int32).cuda(), experts)
+    for dtype, biased in (("bf16", True), ("fp16", False), ("fp32", True)):
+        say("routed product by", kernel, experts, tokens, top, n, k, fan, dtype)
+        bias = _rand(torch, 5, experts, n, dtype=dtype) if biased else None
+        room = torch.full((tokens * top * n + 128,), 77.0, dtype=_dtype(torch, dtype), device="cuda")
+        out = room[64:-64].view(tokens * top, n)
+        cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=per, bias=bias, out=out)
+        assert bool((out[(flat < 0) | (flat >= experts)] == 77.0).all())
+        assert bool((room[:64] == 77.0).all()) and bool((room[-64:] == 77.0).all())
+        for e in range(experts):
+            r = (flat == e).nonzero()[:, 0]
+            at = r // per
+            if r.numel():
+                _check_on_device(torch, out[r], x8[at], dx[at], w8[e], dw[e], None if bias is None else bias[e], dtype, e)

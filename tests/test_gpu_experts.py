@@ -860,3 +860,44 @@ def test_routed_product_by_every_kernel(torch_dev, experts, tokens, top, n, k, k
             at = r // per
             if r.numel():
                 _check_on_device(torch, out[r], x8[at], dx[at], w8[e], dw[e], None if bias is None else bias[e], dtype, e)
+
+
+@pytest.mark.parametrize("rows,fan,dtype", [(65600, 2, "bf16"), (140000, 3, "fp16"), (131200, 1, "fp32")])
+def test_routed_product_of_rows_behind_2_gib(torch_dev, rows, fan, dtype):
+    # several experts, tiles that are full and not, a last step of 16 codes, rows of x up to
+    # the last and behind 4 GiB: the same bits as the dense product of the same rows
+    torch, cq = torch_dev, _cq()
+    experts, n, k = 5, 203, 32784
+    routes = rows * fan
+    assert cq.cq_probe_w8_kernel(rows, n, k, experts, routes, fan) == ("tiles far", 128, 128, 2)
+    say("far rows", rows, fan, dtype)
+    g = torch.Generator().manual_seed(fan)
+    x8 = torch.empty((rows, k), dtype=torch.int8, device="cuda")
+    x8[:100], x8[-400:] = _int8(torch, 1, 100, k), _int8(torch, 2, 400, k)
+    dx, w8, dw = _scales(torch, 3, rows), _int8(torch, 4, experts, n, k), _scales(torch, 5, experts, n)
+    bias = _rand(torch, 6, experts, n, dtype=dtype)
+    chosen = torch.full((rows, fan), -1, dtype=torch.int32)
+    # the second expert has none, the fourth five
+    share = torch.tensor([0, 0, 0, 2, 4], dtype=torch.int32)
+    chosen[-400:] = share[torch.randint(0, 5, (400, fan), generator=g)]
+    chosen[:100] = share[torch.randint(0, 5, (100, fan), generator=g)]
+    chosen[-5:, 0] = 3
+    flat = chosen.flatten().cuda()
+    plan = cq.cq_route_plan(flat, experts)
+    out = torch.full((routes, n), 77.0, dtype=_dtype(torch, dtype), device="cuda")
+    cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=fan, bias=bias, out=out)
+    assert bool((out[flat < 0] == 77.0).all())
+    for e in range(experts):
+        r = (flat == e).nonzero()[:, 0]
+        if r.numel():
+            x, d = x8[r // fan], dx[r // fan]
+            want = cq.cq_gemm_w8(x, d, w8[e].clone(), dw[e].clone(), bias=bias[e].clone(), y_dtype=_dtype(torch, dtype))
+            assert torch.equal(out[r], want), e
+            _check_on_device(torch, out[r], x, d, w8[e], dw[e], bias[e], dtype, e)
+    # offsets that are none
+    # offsets far from each other, between which the third expert has all
+    plan[:experts + 1] = torch.tensor([2**31 - 1, -5, -2**31 + 7, routes, -2**31 + 1, 0], dtype=torch.int32)
+    out.fill_(77.0)
+    x8.fill_(0)
+    cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=fan, out=out)
+    assert bool((out[flat < 0] == 77.0).all()) and not bool(out[flat >= 0].any())

@@ -114,7 +114,8 @@ cq_status cq_gemm_routed_w8(const cq_w8_args *args, void *stream);
 /*
  * cq_gated -- the gated activation between two products (device):
  * h = act(gate) up, with act(v) = v / (1 + exp(-v)), or the GELU by tanh,
- * v / 2 (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).
+ * v / 2 (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).  Formed in FP32: values of act
+ * below 2^-119 in size may be zero.
  * cq_gated_a8: h, rounded to dtype, straight to the carriers of the Dynamic-A8
  * and 8-bit products: x8 int8 [rows, width] and dx float [rows] equal
  * cq_quantize_act_a8 of h bit for bit (width % 32 == 0).  args->out may be NULL.

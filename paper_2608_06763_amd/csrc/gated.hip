@@ -18,8 +18,10 @@ namespace cq {
 
 namespace {
 
-// exp to 2^-22 relative; the quotient's reciprocal to one unit.  exp(-v) of a v
-// below -88 is infinite and its quotient zero, as the activation's value is there.
+// Off by (8 |z| + 16) 2^-24 of the value at most: z by log2 e is rounded, which the
+// exponential turns into an error that grows with |z|; it and the reciprocal are good to a
+// unit or two.  Where e^-z leaves FP32, from z = -87.3 on, the reciprocal may be zero: with
+// it goes at most 2^-119, which BF16 could still hold.
 template <int ACT>
 __device__ __forceinline__ float activate(float v) {
     float z = v;

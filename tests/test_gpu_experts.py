@@ -901,3 +901,23 @@ def test_routed_product_of_rows_behind_2_gib(torch_dev, rows, fan, dtype):
     x8.fill_(0)
     cq.cq_gemm_routed_w8(x8, dx, w8, dw, plan, fan=fan, out=out)
     assert bool((out[flat < 0] == 77.0).all()) and not bool(out[flat >= 0].any())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype,ups", [("bf16", (-0.75, 3.0, 2.0**60, -2.0**100)), ("fp16", (-0.75, 3.0, 1000.0))])
+def test_gated_of_every_value_down_to_the_smallest(torch_dev, act, dtype, ups):
+    # beside the half step of the output and the exponent's error, at most 2^-119 of up is
+    # lost, where e^-v leaves FP32; FP16 has no such value
+    torch, cq = torch_dev, _cq()
+    gate = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(_dtype(torch, dtype)).cuda().view(8, 8192)
+    g, most = _f64(gate), float(torch.finfo(_dtype(torch, dtype)).max)
+    half_step = {"bf16": 2.0**-134, "fp16": 2.0**-25}[dtype]
+    for u in ups:
+        say("gated, small", act, dtype, u)
+        got = _f64(cq.cq_gated(gate, torch.full_like(gate, u), act=act))
+        with np.errstate(invalid="ignore"):
+            ref, z = _gated_ref(np.where(np.isfinite(g), g, 0.0), u, act)
+        ok = np.isfinite(g) & (np.abs(ref) < most)
+        bound = U[dtype] * np.abs(ref) + E * (16.0 + 8.0 * np.minimum(z, 128.0)) * np.abs(ref) + half_step + 2.0**-119 * abs(u)
+        off = np.where(ok, np.abs(got - ref) - bound, -1.0)
+        assert (off <= 0).all(), (u, g.ravel()[np.argmax(off)])

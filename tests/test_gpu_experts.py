@@ -921,3 +921,24 @@ def test_gated_of_every_value_down_to_the_smallest(torch_dev, act, dtype, ups):
         bound = U[dtype] * np.abs(ref) + E * (16.0 + 8.0 * np.minimum(z, 128.0)) * np.abs(ref) + half_step + 2.0**-119 * abs(u)
         off = np.where(ok, np.abs(got - ref) - bound, -1.0)
         assert (off <= 0).all(), (u, g.ravel()[np.argmax(off)])
+
+
+@pytest.mark.parametrize("tokens,experts,top", [(1, 128, 8), (31, 64, 6), (700, 256, 8), (5, 1000, 32), (90, 72, 16)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_route_without_a_plan(torch_dev, tokens, experts, top, biased):
+    # from C, which leaves the plan and its workspace out
+    torch, cq = torch_dev, _cq()
+    from paper_2608_06763_amd import experts as X
+    say("no plan", tokens, experts, top, biased)
+    logits = _rand(torch, 1, tokens, experts, dtype="fp32", scale=2.0)
+    bias = _rand(torch, 2, experts, dtype="fp32", scale=0.1) if biased else None
+    live = torch.tensor([tokens - tokens // 4], dtype=torch.int32, device="cuda")
+    want = cq.cq_route(logits, top, bias=bias, live=live)
+    chosen = torch.full((tokens * top + 8,), -77, dtype=torch.int32, device="cuda")
+    weights = torch.full((tokens * top + 8,), 77.0, device="cuda")
+    args = X._ROUTE.pack(logits.data_ptr(), bias.data_ptr() if biased else 0, live.data_ptr(), chosen.data_ptr(),
+                         weights.data_ptr(), 0, tokens, experts, 2, experts, top, 0, 1, 1, 1, 1, 1.0)
+    assert cq.lib().cq_route_workspace_bytes(args) == 0
+    assert cq.lib().cq_route(args, None, 0, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(chosen[:-8].view(tokens, top), want[0]) and torch.equal(weights[:-8].view(tokens, top), want[1])
+    assert bool((chosen[-8:] == -77).all()) and bool((weights[-8:] == 77.0).all())

@@ -942,3 +942,23 @@ def test_route_without_a_plan(torch_dev, tokens, experts, top, biased):
     assert cq.lib().cq_route(args, None, 0, torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(chosen[:-8].view(tokens, top), want[0]) and torch.equal(weights[:-8].view(tokens, top), want[1])
     assert bool((chosen[-8:] == -77).all()) and bool((weights[-8:] == 77.0).all())
+
+
+@pytest.mark.parametrize("tokens,experts,top", [(70001, 256, 8), (40000, 100, 1), (16385, 1024, 6), (16384, 64, 16), (131072, 12, 3),
+                                                (20000, 60, 20)])
+def test_route_of_many_tokens_equals_its_parts(torch_dev, tokens, experts, top):
+    torch, cq = torch_dev, _cq()
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    logits = torch.randn((tokens, experts), generator=g, device="cuda").to(torch.bfloat16)
+    bias = _rand(torch, 2, experts, dtype="fp32", scale=0.1)
+    live = torch.tensor([tokens - 77], dtype=torch.int32, device="cuda")
+    for kw in (dict(bias=bias, scoring="sigmoid"), dict(), dict(bias=bias, groups=4, kept_groups=2, group_top=2)):
+        if kw.get("groups") and top > experts // 2:
+            continue
+        say("many tokens", tokens, experts, top, sorted(kw))
+        chosen, weights, plan = cq.cq_route(logits, top, live=live, **kw)
+        for t in range(0, tokens, 3000):
+            rest = torch.tensor([max(0, min(3000, tokens - 77 - t))], dtype=torch.int32, device="cuda")
+            part = cq.cq_route(logits[t:t + 3000], top, live=rest, **kw)
+            assert torch.equal(chosen[t:t + 3000], part[0]) and torch.equal(weights[t:t + 3000], part[1]), t
+        assert np.array_equal(plan.cpu().numpy(), _plan_ref(chosen.cpu().numpy(), experts))

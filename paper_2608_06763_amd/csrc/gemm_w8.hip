@@ -66,9 +66,10 @@ w8::choice dense(const w8::params &p) {
             least = cost;
         }
     }
-    // Few rows of few channels: K shared out over a workgroup's waves, whose stage is a step
-    // of each wave's eighth of K (45 rows of 4096 x 14336 19 us, in tiles 50; 48 of 14336 x
-    // 4096 29 and 20).  Up to 16 rows that is the better kernel for all.
+    // Where tiles would leave the card empty, however many rows: K shared out over a
+    // workgroup's waves, whose stage is a step of each wave's eighth of K (weights from memory,
+    // us: 45 rows of 4096 x 14336 18.6, in tiles 50; 48 of 14336 x 4096 28 and 20; 1300 of 384 x
+    // 5872 20.8 and 23).  Up to 16 rows that is the better kernel for all.
     if (p.rows <= 16 || 1.0 + 0.2 * stages * std::max(1.0, cells(32, 32) / 256.0) < least) return w8::rows_choice(p);
     return tiles(*best);
 }
@@ -78,10 +79,10 @@ w8::choice routed(const w8::params &p) {
     // routes of an expert, were all taken alike
     const double each = double(p.routes) / p.experts;
     if (each <= 5.0) return w8::few_rows_choice(p, true);
-    // 128 experts of 2048 x 2048, us: 6 routes each 102 in tiles of 64 x 128 (109 by the few
-    // rows' kernel), 37 each 140 (64 x 256: 140), 62 each 162 (151); 64 experts of 4096 x
-    // 4096: 62 each 292 (267; 128 x 256: 257), 250 each 469 in 128 x 256 (256 x 256: 473),
-    // 500 each 753 (728).
+    // 128 experts of 2048 x 2048, us: 6 routes each 102 in tiles of 64 x 128 (117 by the few
+    // rows' kernel), 37 each 139 (64 x 256: 140), 62 each 161 (150); 64 experts of 4096 x
+    // 4096: 62 each 289 (265; 128 x 256: 267), 250 each 468 in 128 x 256 (256 x 256: 488),
+    // 500 each 773 (739).
     // With short rows tiles that share a compute unit hide each other's way in and out.
     const bool brief = p.k <= 1024 && each > 80.0;
     const int m = each <= 80.0 ? 64 : each < 400.0 || brief ? 128 : 256, n = each <= 40.0 || brief ? 128 : 256;

@@ -8,11 +8,13 @@
 // registers.  There neighbouring lanes hold different rows, as the matrix cores want them,
 // and the caches serve 16 bytes a cycle and compute unit; repeated rows cost little.  With
 // more rows (w8_rows) each wave brings its steps straight into its own part of LDS, whole
-// cache lines a row, at up to 64 bytes a cycle: 45 rows of 4096 x 14336 32 -> 19 us.
+// cache lines a row, at up to 64 bytes a cycle: 45 rows of 4096 x 14336 40 -> 18.6 us.
 //
-// Measured: 1 row of 28672 x 8192 41 us, 5.7 TB/s (a sum over 2 GiB: 6.1), of 6144 x 4096
-// 8.5 us; 8 experts of 64 for one token, 4096 x 2048 each, 15.7 us, 4.3 TB/s; 61 tokens of
-// 6 experts of 96, 2048 x 1408 each, 55 us, 4.7 TB/s.
+// Measured, weights from memory: 1 row of 28672 x 8192 41 us, 5.8 TB/s (a sum over 2 GiB:
+// 6.1), of 6144 x 4096 9.4 us; 8 experts of 64 for one token, 4096 x 2048 each, 16.2 us, 4.2
+// TB/s; 61 tokens of 6 experts of 96, 2048 x 1408 each, 57 us, 4.6 TB/s.  Where the weights
+// are still in the card's last cache 7.7 us for the 6144 x 4096, 14 for the 45 rows above and
+// for the 8 experts.
 #include "gemm_w8.h"
 
 namespace cq {

@@ -15,11 +15,13 @@
 //
 // What bounds it: 256 x 256 tiles the card's power.  8192^3 443 us, 2480 TOP/s (a library's
 // product of these integers 2480), the matrix cores busy for 65% of the cycles at 1.77 GHz, no
-// bank conflicts; with operands always in the nearest cache 431.  7013 x 28672 x 8192 1.41 to
-// 1.46 ms, 2250 to 2330 TOP/s.  Routed: 8191 tokens of 4 experts of 48, 4096 x 4096, 692 us,
-// 1590 TOP/s, as tiles that an expert's last routes fill in part cost whole ones (a path of half
-// the rows for them gave 1%).  Small tiles wait for memory: 512 x 4096 x 4096 14.2 us with four
-// stages in flight, 22 with two.
+// bank conflicts; with operands always in the nearest cache 431.  (Cards differ: others take
+// 462 to 468 us.)  7013 x 28672 x 8192 1.41 to 1.49 ms, 2210 to 2330 TOP/s.  Routed: 8191 tokens
+// of 4 experts of 48, 4096 x 4096, 670 to 706 us, 1560 to 1640 TOP/s, as tiles that an expert's
+// last routes fill in part cost whole ones (a path of half the rows for them gave 1%), and as a
+// tile's way in and out, by the fit in gemm_w8.hip a fifth of its time with 32 stages, has
+// nothing beside it: the tile fills its compute unit.  Small tiles wait for memory: 512 x 4096 x
+// 4096 15.5 us with four stages in flight, 21.4 with two.
 #pragma once
 
 #include "gemm_w8.h"

@@ -273,12 +273,13 @@ __device__ __forceinline__ double inverse(double v) {
 }
 
 // e^x to 2^-50, without a branch, so that a lane's experts run beside each other: 2^n e^r
-// with |r| <= ln 2 / 2 and e^r by its series up to r^13 (what is left is below 2^-57).
+// with |r| <= ln 2 / 2 (ln 2 in two parts: Cody and Waite's reduction) and e^r by its series
+// up to r^13 (what is left is below 2^-57).
 // Beyond -746 .. 709, where FP64 has no values, the nearest of these.
 __device__ __forceinline__ double exp64(double x) {
     x = fmin(fmax(x, -746.0), 709.0);
     const double n = __builtin_rint(x * 1.4426950408889634);
-    // ln 2 in two parts, the first short enough for n times it to be exact
+    // the first part is short enough for n times it to be exact
     const double r = __builtin_fma(n, -1.9082149292705877e-10, __builtin_fma(n, -0.69314718036912382, x));
     double s = 1.0 / 6227020800.0;
     s = __builtin_fma(s, r, 1.0 / 479001600.0);

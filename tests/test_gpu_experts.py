@@ -962,3 +962,68 @@ def test_route_of_many_tokens_equals_its_parts(torch_dev, tokens, experts, top):
             part = cq.cq_route(logits[t:t + 3000], top, live=rest, **kw)
             assert torch.equal(chosen[t:t + 3000], part[0]) and torch.equal(weights[t:t + 3000], part[1]), t
         assert np.array_equal(plan.cpu().numpy(), _plan_ref(chosen.cpu().numpy(), experts))
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_route_of_infinities_by_every_search(torch_dev, scoring, dtype):
+    # the exact search alone (more than twelve choices) and a wave a token (more than sixteen
+    # choices, or groups)
+    torch = torch_dev
+    inf, nan = float("inf"), float("nan")
+    low, most = torch.finfo(_dtype(torch, dtype)).min, torch.finfo(_dtype(torch, dtype)).max
+    logits = _rand(torch, 44, 13, 96, dtype=dtype)
+    logits[0], logits[1] = -inf, nan
+    logits[2, ::2], logits[3, 1::3] = -inf, nan
+    logits[4, 5], logits[4, 50] = inf, inf
+    logits[5] = low
+    logits[6] = -inf
+    logits[6, 95] = 1.0
+    logits[7, :94] = nan
+    logits[8, 3:] = low
+    logits[9] = inf
+    logits[10, 10:] = -60.0
+    logits[11, ::7] = most
+    bias = _rand(torch, 45, 96, dtype="fp32", scale=0.1)
+    odd = bias.clone()
+    odd[:40], odd[40], odd[41], odd[50:70] = -inf, nan, inf, torch.finfo(torch.float32).min
+    for n, (top, opt) in enumerate([(14, dict(bias=bias)), (16, dict(bias=odd)), (15, dict()), (20, dict()), (20, dict(bias=odd)),
+                                    (32, dict(renormalize=False)), (6, dict(groups=32, kept_groups=5, group_top=2)),
+                                    (6, dict(groups=32, kept_groups=9, group_top=2, bias=odd)),
+                                    (14, dict(groups=12, kept_groups=4, group_top=2, bias=odd)),
+                                    (6, dict(groups=48, kept_groups=3, bias=bias)), (6, dict(groups=48, kept_groups=3))]):
+        say("route odd values, searches", scoring, dtype, n)
+        _check_route(torch, logits, top, n, scoring=scoring, **opt)
+
+
+@pytest.mark.parametrize("width", [64, 1024, 4096, 14336])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_gated_to_carriers_of_odd_values(torch_dev, width, dtype):
+    torch, cq = torch_dev, _cq()
+    gate, up = _rand(torch, 1, 9, width, dtype=dtype, scale=3.0), _rand(torch, 2, 9, width, dtype=dtype)
+    inf, info = float("inf"), torch.finfo(_dtype(torch, dtype))
+    gate[0, 3], gate[1, 5], gate[2] = inf, float("nan"), -inf
+    up[3, 7], up[4, ::9], gate[5] = -inf, float("nan"), 0.0
+    gate[6], up[6] = info.max, info.max
+    gate[7], up[7] = info.tiny, info.tiny
+    up[8, :-1] = info.smallest_normal
+    for act in ("silu", "gelu"):
+        say("gated a8, odd values", width, dtype, act)
+        h = torch.empty_like(gate)
+        x8, dx = cq.cq_gated_a8(gate, up, act=act, out=h)
+        assert torch.equal(h.view(torch.int16), cq.cq_gated(gate, up, act=act).view(torch.int16))
+        want8, wantx = cq.cq_quantize_act_a8(h)
+        assert torch.equal(x8, want8) and torch.equal(dx.view(torch.int32), wantx.view(torch.int32))
+
+
+def test_combine_of_odd_values(torch_dev):
+    # routes without an expert give nothing, whatever their weights and rows hold; others
+    # what the sum gives
+    torch, cq = torch_dev, _cq()
+    inf, nan = float("inf"), float("nan")
+    y = torch.ones((5 * 3, 16), dtype=torch.bfloat16, device="cuda")
+    chosen = torch.tensor([[-1, 7, 2**31 - 1], [0, -2**31, 1], [2, 2, 2], [3, 0, 1], [-1, -1, -1]], dtype=torch.int32, device="cuda")
+    weights = torch.tensor([[nan, inf, -inf], [0.5, nan, 0.25], [1.0, 2.0, 4.0], [inf, 1.0, 1.0], [nan] * 3], device="cuda")
+    y[:3], y[4] = nan, inf
+    got = cq.cq_combine(y, weights, chosen, 4, out=torch.empty((5, 16), device="cuda"))
+    assert torch.equal(got, torch.tensor([0.0, 0.75, 7.0, inf, 0.0], device="cuda")[:, None].expand(5, 16))
